@@ -215,6 +215,115 @@ int clear_qk_norm_rope(const void *q_in, const void *k_in, void *q_out, void *k_
                        int axis0_dim, int axis1_dim, int axis2_dim, float theta, float ntk_factor, float eps,
                        float q_factor, void *stream);
 
+/* Gradient of clear_qk_norm_rope.  q, k: the inputs of that call; dq_rot, dk_rot: the gradients of its outputs (those of
+ * clear_attn_bwd_*); dq, dk: the gradients of q and k; the other arguments as in that call.  With u the upstream gradient turned
+ * back (and times q_factor), inv = 1 / sqrt(mean_c(x_c^2) + eps) and s = u * gain:
+ *     dx = inv * (s - x * inv^2 * mean_c(s_c x_c)),      dgain_c = sum over b, h, n of u_c x_c inv.
+ * dgain_q, dgain_k: head_dim fp32 values each, or NULL; they are written, not added to.  All seven tensors have one dtype and the
+ * layout of clear_qk_norm_rope; dq may lie in the place of q or of dq_rot, dk in that of k or of dk_rot, any other overlap is not
+ * allowed.  fp32 arithmetic; sums in a fixed order, so repeats on one kind of device are equal bit for bit.
+ * workspace: clear_qk_norm_rope_bwd_workspace() bytes of device memory, 16-byte aligned, which the call may write until it has
+ * ended on the stream (calls that can overlap need one each); may be NULL when neither gain's gradient is wanted.
+ * One launch on `stream`, two with a gain's gradient; no allocation, no host synchronisation.
+ * Errors: those of clear_qk_norm_rope; INVALID_ARG also for a workspace that is missing or too small. */
+int clear_qk_norm_rope_bwd(const void *q, const void *k, const void *dq_rot, const void *dk_rot, void *dq, void *dk,
+                           const float *gain_q, const float *gain_k, float *dgain_q, float *dgain_k, int B, int H, int grid_h,
+                           int grid_w, int n_text, int head_dim, int dtype, int axis0_dim, int axis1_dim, int axis2_dim, float theta,
+                           float ntk_factor, float eps, float q_factor, void *workspace, size_t workspace_bytes, void *stream);
+
+/* Bytes of that workspace on the current device.  Errors: INVALID_ARG, UNSUPPORTED (head_dim other than 64 or 128), CUDA. */
+int clear_qk_norm_rope_bwd_workspace(int head_dim, size_t *bytes);
+
+/* Pair layouts of the rotary embedding, and how its frequencies are scaled for sequences longer than those of training. */
+enum {
+    CLEAR_ROPE_INTERLEAVED = 0, /* pair p = channels (2p, 2p + 1)                                             */
+    CLEAR_ROPE_HALF = 1         /* pair p = channels (p, p + P), P pairs in the rotary part of the head       */
+};
+enum {
+    CLEAR_ROPE_SCALE_NONE = 0,
+    CLEAR_ROPE_SCALE_LINEAR = 1, /* every frequency divided by the factor (positions interpolated)            */
+    CLEAR_ROPE_SCALE_NTK = 2,    /* the base times factor^(dim/(dim-2)): the highest frequency stays, the
+                                    lowest is divided by the factor                                           */
+    CLEAR_ROPE_SCALE_PARTS = 3   /* by parts (arXiv 2309.00071, Sec. 3.2): frequencies of at least `fast` turns
+                                    within the trained length stay, those of at most `slow` turns are divided by
+                                    the factor, those between are blended linearly in the number of turns     */
+};
+
+/* Angular frequencies of a group of dim channels: frequencies[k] = theta^(-2k/dim), k < dim/2, scaled as said above.  Host memory,
+ * no CUDA call.  trained_length, fast and slow are read by CLEAR_ROPE_SCALE_PARTS only.  The attention factor that goes with that
+ * scaling, 0.1 ln(factor) + 1 on Q and on K, is `factor` of clear_rope_fwd.
+ * Errors: INVALID_ARG (a null pointer, dim odd or <= 0, theta, factor or trained_length <= 0, fast <= slow, slow < 0, a non-finite
+ * value, an unknown scaling). */
+int clear_rope_frequencies(double *frequencies, int dim, double theta, int scaling, double factor, double trained_length,
+                           double fast, double slow);
+
+/* Rotary positions of Q and K.  For every batch entry b, head h and token n, pair p of the first rotary_dim = sum(axes_dim)
+ * channels turns by the angle t = positions[b, n, a(p)] * frequencies[p], a(p) the axis whose group holds pair p (the axes' groups
+ * follow one another, axes_dim[a] / 2 pairs each):
+ *     first_p = factor * (x_first cos t - x_second sin t),   second_p = factor * (x_first sin t + x_second cos t);
+ * the head's other channels are copied unchanged.  clear_rope_bwd is the gradient: the same with -t (q, k: gradients of the rotated
+ * tensors; q_out, k_out: those of the tensors before).
+ * q, q_out: [B, H, N, head_dim]; k, k_out: [B, Hk, N, head_dim], or both NULL; device memory, bf16 or fp32, channels contiguous,
+ * the other three axes with strides of any sign in elements: `strides` holds the (b, h, n) strides of q, q_out, k, k_out in this
+ * order (twelve values, host memory; the last six are not read without k), so that Q and K may be read out of one packed projection
+ * and written head by head.  An output may be its own input with the same strides (in place); any other overlap of an output with an
+ * input or an output is not allowed, nor are an output's own rows to overlap.
+ * positions: device memory, int32 or int64 (position_bits 32 or 64), [B, N, n_axes] with the last axis contiguous; pos_stride_b
+ * is 0 where all batch entries share them.  Any value: the angle is taken modulo a turn in 64-bit fixed point, so far positions lose
+ * nothing.  frequencies: host memory, rotary_dim / 2 values (as clear_rope_frequencies gives them, or any others).
+ * fp32 arithmetic.  One launch on `stream`, no allocation, no host synchronisation.  B or N of zero: nothing is done.
+ * Errors: INVALID_ARG (a negative size, H <= 0, Hk <= 0 with k, an axis' group odd or negative, no pair at all, rotary_dim above
+ * head_dim, a non-finite frequency or factor, unknown layout, dtype or position_bits, a null pointer, k without k_out, an output
+ * that is its own input under other strides, that is the other output or the other input, or whose rows fall on one another by a
+ * stride of zero), UNSUPPORTED (head_dim > 256, n_axes > 8, more than 2^31 - 1 blocks), MISALIGNED (a pointer that is not a
+ * multiple of its element), CUDA. */
+int clear_rope_fwd(const void *q, const void *k, void *q_out, void *k_out, const long long *strides, const void *positions,
+                   long long pos_stride_b, long long pos_stride_n, int position_bits, const double *frequencies,
+                   const int *axes_dim, int n_axes, int B, int H, int Hk, int N, int head_dim, int dtype, int layout, float factor,
+                   void *stream);
+int clear_rope_bwd(const void *q, const void *k, void *q_out, void *k_out, const long long *strides, const void *positions,
+                   long long pos_stride_b, long long pos_stride_n, int position_bits, const double *frequencies,
+                   const int *axes_dim, int n_axes, int B, int H, int Hk, int N, int head_dim, int dtype, int layout, float factor,
+                   void *stream);
+
+/* Layer normalisation of the rows of x, [B, N, C]:
+ *     y = (x - mean) * rstd * (weight_offset + weight) + bias,   rstd = 1 / sqrt(mean((x - mean)^2) + eps).
+ * weight, bias: C values each (strides 0), or C values a batch entry (weight_stride_b, bias_stride_b); NULL stands for a gain of one
+ * (whatever weight_offset) and a bias of zero.  A modulated layer passes its scale as weight with weight_offset 1, and its shift.
+ * x, y: device memory, bf16 or fp32, channels contiguous, strides of the batch entries and rows in elements; y may be x with the same
+ * strides, any other overlap is not allowed.  param_dtype: the type of weight and bias, fp32 or that of x.  mean, rstd: [B, N] fp32
+ * contiguous, written for the backward pass, or NULL.  fp32 arithmetic, two passes over a row's registers, so an offset common to a
+ * row costs no accuracy.  One launch on `stream`, no allocation, no host synchronisation.  B or N of zero: nothing is done.
+ * Errors: INVALID_ARG (a negative size, C <= 0, a null x or y, unknown types, param_dtype bf16 with fp32 x, eps < 0, a non-finite
+ * value, y equal to x under other strides, rows of y that fall on one another by a stride of zero), UNSUPPORTED (2^31 rows or
+ * more), MISALIGNED (a pointer that is not a multiple of its element), CUDA. */
+int clear_layer_norm_fwd(const void *x, void *y, const void *weight, const void *bias, float *mean, float *rstd, int B, int N, int C,
+                         int dtype, int param_dtype, long long x_stride_b, long long x_stride_n, long long y_stride_b,
+                         long long y_stride_n, long long weight_stride_b, long long bias_stride_b, float weight_offset, float eps,
+                         void *stream);
+
+/* Gradient of clear_layer_norm_fwd.  mean, rstd: what that call wrote.  With h = (x - mean) * rstd and g = dy * (weight_offset +
+ * weight) (g = dy where weight is NULL):
+ *     dx = rstd * (g - mean_c(g) - h * mean_c(g h)),   dweight = sum over rows of dy h,   dbias = sum over rows of dy,
+ * over the rows of each batch entry where per_batch is not zero (weight [B, C] with weight_stride_b, dweight and dbias [B, C] with
+ * their strides), over all rows otherwise (weight, dweight, dbias [C], strides 0).  dweight, dbias: of param_dtype, written, not
+ * added to; either may be NULL.  dx may lie in the place of x or of dy with the same strides; any other overlap is not allowed.
+ * fp32 arithmetic; sums in a fixed order, so repeats on one kind of device are equal bit for bit.
+ * workspace: clear_layer_norm_bwd_workspace() bytes of device memory, 16-byte aligned, which the call may write until it has ended on
+ * the stream (calls that can overlap need one each); may be NULL when neither sum is wanted.  One launch on `stream`, two with a sum
+ * (three above 8192 channels); no allocation, no host synchronisation.  Without rows dweight and dbias are set to zero.
+ * Errors: those of clear_layer_norm_fwd; INVALID_ARG also for missing statistics, for a workspace that is missing or too small, for
+ * strides of weight, dweight or dbias that do not go with per_batch; UNSUPPORTED also for more than 65535 batch entries with
+ * per_batch. */
+int clear_layer_norm_bwd(const void *x, const void *dy, const void *weight, const float *mean, const float *rstd, void *dx,
+                         void *dweight, void *dbias, int B, int N, int C, int dtype, int param_dtype, int per_batch,
+                         long long x_stride_b, long long x_stride_n, long long dy_stride_b, long long dy_stride_n,
+                         long long dx_stride_b, long long dx_stride_n, long long weight_stride_b, long long dweight_stride_b,
+                         long long dbias_stride_b, float weight_offset, void *workspace, size_t workspace_bytes, void *stream);
+
+/* Bytes of that workspace on the current device.  Errors: INVALID_ARG, UNSUPPORTED, CUDA. */
+int clear_layer_norm_bwd_workspace(int B, int N, int C, int per_batch, size_t *bytes);
+
 /* sqrt(log n_tokens / log n_train_tokens): the factor on the logits that keeps the entropy of the attention
  * of a longer sequence where it was at the training length (the log-scale attention factor Sec. 4.3 applies
  * beyond the training resolution).  Host arithmetic only; 1 when either count is below 2. */

@@ -7,6 +7,7 @@ fallback: if the library cannot be loaded, or a call fails, a ``ClearError`` is 
 from __future__ import annotations
 
 import ctypes
+import functools
 import os
 import threading
 from typing import Optional
@@ -21,6 +22,8 @@ KERNEL_AUTO, KERNEL_SIMT, KERNEL_TCGEN05, KERNEL_TCGEN05_WS = 0, 1, 2, 3
 MASK_DISC, MASK_SQUARE, MASK_WINDOWS, MASK_STRIDED = 0, 1, 2, 3
 PART_ALL, PART_BAND_IMAGE, PART_BAND_TEXT = 0, 1, 2
 TEXT_MERGE_EXACT, TEXT_MERGE_AVERAGE = 0, 1
+ROPE_INTERLEAVED, ROPE_HALF = 0, 1
+ROPE_SCALE_NONE, ROPE_SCALE_LINEAR, ROPE_SCALE_NTK, ROPE_SCALE_PARTS = 0, 1, 2, 3
 TILE_LINEAR, TILE_MASKED = 1, 2
 STEP_USE0, STEP_USE1, STEP_SHARED, STEP_LINEAR, STEP_MASKED0, STEP_MASKED1 = 1, 2, 4, 8, 16, 32
 STEP_CLIP0, STEP_CLIP1 = 64, 128
@@ -34,6 +37,8 @@ EXPORTS = [
     "clear_qk_norm_rope", "clear_log_scale_factor",
     "clear_band_geometry", "clear_plan_create_band", "clear_attn_text_partial", "clear_text_merge",
     "clear_plan_create_mask", "clear_attn_bwd_bf16", "clear_attn_bwd_bf16_tc", "clear_plan_side_words",
+    "clear_qk_norm_rope_bwd", "clear_qk_norm_rope_bwd_workspace", "clear_rope_frequencies", "clear_rope_fwd", "clear_rope_bwd",
+    "clear_layer_norm_fwd", "clear_layer_norm_bwd", "clear_layer_norm_bwd_workspace",
 ]
 
 
@@ -108,6 +113,15 @@ def load() -> ctypes.CDLL:
         lib.clear_attn_text_partial.argtypes = [vp, vp, vp, vp, vp, f32, vp]
         lib.clear_plan_create_mask.argtypes = [ctypes.POINTER(vp), i32, i32, i32, i32, i32, i32, i32, i32, f32, i32, i32]
         lib.clear_text_merge.argtypes = [vp, i32, i32, i32, i32, i32, i32, vp, ctypes.c_longlong, vp]
+        i64, f64, size, psize = ctypes.c_longlong, ctypes.c_double, ctypes.c_size_t, ctypes.POINTER(ctypes.c_size_t)
+        lib.clear_qk_norm_rope_bwd.argtypes = [vp] * 10 + [i32] * 10 + [f32] * 4 + [vp, size, vp]
+        lib.clear_qk_norm_rope_bwd_workspace.argtypes = [i32, psize]
+        lib.clear_rope_frequencies.argtypes = [vp, i32, f64, i32, f64, f64, f64, f64]
+        lib.clear_rope_fwd.argtypes = [vp, vp, vp, vp, vp, vp, i64, i64, i32, vp, vp] + [i32] * 8 + [f32, vp]
+        lib.clear_rope_bwd.argtypes = lib.clear_rope_fwd.argtypes
+        lib.clear_layer_norm_fwd.argtypes = [vp] * 6 + [i32] * 5 + [i64] * 6 + [f32, f32, vp]
+        lib.clear_layer_norm_bwd.argtypes = [vp] * 8 + [i32] * 6 + [i64] * 9 + [f32, vp, size, vp]
+        lib.clear_layer_norm_bwd_workspace.argtypes = [i32, i32, i32, i32, psize]
         lib.clear_log_scale_factor.argtypes = [ctypes.c_longlong, ctypes.c_longlong]
         lib.clear_log_scale_factor.restype = f32
         plan_args = [ctypes.POINTER(vp), i32, i32, i32, i32, i32, i32, f32, i32, i32]
@@ -249,6 +263,221 @@ def clear_qk_norm_rope(q, k, q_out, k_out, grid_h, grid_w, n_text, axes_dim, gai
                                      a0, a1, a2, float(theta), float(ntk_factor), float(eps), float(q_factor),
                                      _stream_ptr(stream)), "clear_qk_norm_rope")
     return q_out, k_out
+
+
+def _on_device_of(t, stream, call):
+    """``call(stream pointer)`` with the device of ``t`` current; its current stream unless one is given."""
+    import torch
+    index = t.device.index
+    if index != torch.cuda.current_device():
+        with torch.cuda.device(index):
+            return _on_device_of(t, stream, call)
+    return call(torch._C._cuda_getCurrentRawStream(index) if stream is None else _stream_ptr(stream))
+
+
+def _workspace(n_bytes, device, stream_ptr):
+    """Device memory for one call on that stream: torch's allocator keeps it from other streams until the call has ended."""
+    import torch
+    if stream_ptr == torch._C._cuda_getCurrentRawStream(device.index):
+        return torch.empty(n_bytes, dtype=torch.uint8, device=device)
+    with torch.cuda.stream(torch.cuda.ExternalStream(stream_ptr, device=device)):
+        return torch.empty(n_bytes, dtype=torch.uint8, device=device)
+
+
+@functools.lru_cache(maxsize=256)
+def _workspace_bytes(fn_name, device_index, *shape):
+    out = ctypes.c_size_t()
+    _check(getattr(load(), fn_name)(*shape, ctypes.byref(out)), fn_name)
+    return out.value
+
+
+def _ptr(t):
+    return None if t is None else t.data_ptr()
+
+
+def clear_qk_norm_rope_bwd(q, k, dq_rot, dk_rot, dq, dk, grid_h, grid_w, n_text, axes_dim, gain_q=None, gain_k=None, dgain_q=None,
+                           dgain_k=None, theta=10000.0, ntk_factor=1.0, eps=1e-6, q_factor=1.0, stream=None):
+    """Gradient of ``clear_qk_norm_rope``: from its inputs ``q``, ``k`` and the gradients ``dq_rot``, ``dk_rot`` of its outputs into
+    ``dq``, ``dk`` and, where given, the gains' ``dgain_q``, ``dgain_k`` (fp32, head_dim values).  Returns the four."""
+    import torch
+    dtype, shape, device = q.dtype, q.shape, q.device
+    for t in (q, k, dq_rot, dk_rot, dq, dk):
+        if not (t.is_cuda and t.is_contiguous() and t.dtype == dtype and t.shape == shape and t.device == device):
+            raise ValueError("q, k and the gradients must be contiguous CUDA tensors of one dtype, device and [B, H, N, d] shape")
+    if dtype not in (torch.bfloat16, torch.float32):
+        raise ValueError("bf16 or fp32 tensors")
+    if len(shape) != 4 or shape[2] != n_text + grid_h * grid_w:
+        raise ValueError("q must be [B, H, n_text + grid_h * grid_w, d]")
+    B, H, _, d = shape
+    for g in (gain_q, gain_k, dgain_q, dgain_k):
+        if g is not None and not (g.is_contiguous() and g.dtype == torch.float32 and g.numel() == d and g.device == device):
+            raise ValueError("a gain and its gradient are contiguous fp32 tensors of head_dim values on the device of q")
+    a0, a1, a2 = axes_dim
+
+    def call(st):
+        n_bytes = 0 if dgain_q is None and dgain_k is None else _workspace_bytes("clear_qk_norm_rope_bwd_workspace", device.index, d)
+        ws = _workspace(n_bytes, device, st) if n_bytes else None
+        _check(load().clear_qk_norm_rope_bwd(q.data_ptr(), k.data_ptr(), dq_rot.data_ptr(), dk_rot.data_ptr(), dq.data_ptr(),
+                                             dk.data_ptr(), _ptr(gain_q), _ptr(gain_k), _ptr(dgain_q), _ptr(dgain_k), B, H, grid_h,
+                                             grid_w, n_text, d, BF16 if dtype == torch.bfloat16 else F32, a0, a1, a2, theta,
+                                             ntk_factor, eps, q_factor, _ptr(ws), n_bytes, st), "clear_qk_norm_rope_bwd")
+
+    _on_device_of(q, stream, call)
+    return dq, dk, dgain_q, dgain_k
+
+
+def clear_rope_frequencies(dim, theta=10000.0, scaling=ROPE_SCALE_NONE, factor=1.0, trained_length=1.0, fast=32.0, slow=1.0):
+    """Angular frequencies of a group of ``dim`` channels (a float64 CPU tensor of dim / 2 values), scaled for sequences ``factor``
+    times as long as those of training.  Concatenate the groups of several axes for ``clear_rope_fwd``."""
+    import torch
+    out = torch.empty(max(0, int(dim) // 2), dtype=torch.float64)
+    buf = out.data_ptr() if out.numel() else None
+    _check(load().clear_rope_frequencies(buf, int(dim), float(theta), int(scaling), float(factor), float(trained_length), float(fast),
+                                         float(slow)), "clear_rope_frequencies")
+    return out
+
+
+@functools.lru_cache(maxsize=64)
+def _int_array(values):
+    return (ctypes.c_int * len(values))(*values)
+
+
+def _rope(fn_name, q, k, q_out, k_out, positions, frequencies, axes_dim, layout, factor, stream):
+    import torch
+    dtype, shape, device = q.dtype, q.shape, q.device
+    if dtype not in (torch.bfloat16, torch.float32) or not q.is_cuda or len(shape) != 4:
+        raise ValueError("q must be a bf16 or fp32 CUDA tensor [B, H, N, d]")
+    if (k is None) != (k_out is None):
+        raise ValueError("k and k_out come together")
+    B, H, N, d = shape
+    strides = []
+    for t, t_out in ((q, q_out), (k, k_out)) if k is not None else ((q, q_out),):
+        if t.shape != t_out.shape or t.dim() != 4 or t.shape[0] != B or t.shape[2] != N or t.shape[3] != d:
+            raise ValueError("q, q_out must share one [B, H, N, d] shape, k, k_out one [B, Hk, N, d] shape")
+        for u in (t, t_out):
+            if u.dtype != dtype or u.device != device:
+                raise ValueError("q, k and the outputs must have one dtype and device")
+            sb, sh, sn, sc = u.stride()
+            if sc != 1 and d > 1:
+                raise ValueError("the channels of a head must be contiguous")
+            strides += (sb, sh, sn)
+    axes_dim = tuple(axes_dim)
+    if positions.dtype not in (torch.int32, torch.int64) or positions.device != device or positions.dim() != 3 \
+            or positions.shape[0] not in (1, B) or positions.shape[1] != N or positions.shape[2] != len(axes_dim):
+        raise ValueError("positions must be int32 or int64 [B or 1, N, axes] on the device of q")
+    pb, pn, pa = positions.stride()
+    if pa != 1 and len(axes_dim) > 1:
+        raise ValueError("the axes of a position must be contiguous")
+    if frequencies.dtype != torch.float64 or frequencies.is_cuda or not frequencies.is_contiguous() \
+            or 2 * frequencies.numel() != sum(axes_dim):
+        raise ValueError("frequencies must be a contiguous float64 CPU tensor of sum(axes_dim) / 2 values")
+
+    def call(st):
+        _check(getattr(load(), fn_name)(
+            q.data_ptr(), _ptr(k), q_out.data_ptr(), _ptr(k_out), (ctypes.c_longlong * len(strides))(*strides), positions.data_ptr(),
+            0 if positions.shape[0] == 1 else pb, pn, 32 if positions.dtype == torch.int32 else 64, frequencies.data_ptr(),
+            _int_array(axes_dim), len(axes_dim), B, H, 0 if k is None else k.shape[1], N, d,
+            BF16 if dtype == torch.bfloat16 else F32, layout, factor, st), fn_name)
+
+    _on_device_of(q, stream, call)
+    return (q_out, k_out) if k is not None else q_out
+
+
+def clear_rope_fwd(q, k, q_out, k_out, positions, frequencies, axes_dim, layout=ROPE_INTERLEAVED, factor=1.0, stream=None):
+    """Rotary positions of ``q`` [B, H, N, d] and ``k`` [B, Hk, N, d] (or None) into ``q_out``, ``k_out``: bf16 or fp32 CUDA tensors
+    with any strides but contiguous channels, an output may be its own input.  The first ``sum(axes_dim)`` channels turn by
+    ``positions`` [B or 1, N, axes] (int32 or int64) times ``frequencies`` (float64 on the CPU, as ``clear_rope_frequencies`` gives
+    them), times ``factor``; the others are copied."""
+    return _rope("clear_rope_fwd", q, k, q_out, k_out, positions, frequencies, axes_dim, layout, factor, stream)
+
+
+def clear_rope_bwd(dq_rot, dk_rot, dq, dk, positions, frequencies, axes_dim, layout=ROPE_INTERLEAVED, factor=1.0, stream=None):
+    """Gradient of ``clear_rope_fwd``: from the gradients of the rotated tensors into those of the tensors before."""
+    return _rope("clear_rope_bwd", dq_rot, dk_rot, dq, dk, positions, frequencies, axes_dim, layout, factor, stream)
+
+
+def _norm_rows(x, *others):
+    """(B, N, C) and the (batch entry, row) strides of tensors [N, C] or [B, N, C] that share x's shape, dtype and device."""
+    import torch
+    shape, dtype, device = x.shape, x.dtype, x.device
+    if dtype not in (torch.bfloat16, torch.float32) or not x.is_cuda or len(shape) not in (2, 3):
+        raise ValueError("x must be a bf16 or fp32 CUDA tensor [N, C] or [B, N, C]")
+    strides = []
+    for t in (x, *others):
+        if t.shape != shape or t.dtype != dtype or t.device != device:
+            raise ValueError("x, y and the gradients of rows must share one shape, dtype and device")
+        s = t.stride()
+        if s[-1] != 1 and shape[-1] > 1:
+            raise ValueError("the channels of a row must be contiguous")
+        strides += (0, s[0]) if len(shape) == 2 else (s[0], s[1])
+    return ((1, *shape) if len(shape) == 2 else tuple(shape)), strides
+
+
+def _norm_params(x, B, C, *params):
+    """(dtype code, strides) of weights and biases [C] or [B, C]; None stands for none."""
+    import torch
+    kind, strides = None, []
+    for p in params:
+        if p is None:
+            strides.append(0)
+            continue
+        if p.device != x.device or (p.dtype != torch.float32 and p.dtype != x.dtype) or (kind is not None and p.dtype != kind):
+            raise ValueError("weight, bias and their gradients must have one dtype, fp32 or that of x, and the device of x")
+        if p.dim() not in (1, 2) or p.shape[-1] != C or (p.dim() == 2 and p.shape[0] != B):
+            raise ValueError("weight, bias and their gradients must be [C] or [B, C]")
+        if p.stride(-1) != 1 and C > 1:
+            raise ValueError("the channels of a weight or bias must be contiguous")
+        kind = p.dtype
+        strides.append(p.stride(0) if p.dim() == 2 else 0)
+    return (BF16 if kind == torch.bfloat16 else F32), strides
+
+
+def _norm_stats(x, B, N, *stats):
+    import torch
+    for t in stats:
+        if t is not None and not (t.device == x.device and t.dtype == torch.float32 and t.is_contiguous() and t.numel() == B * N):
+            raise ValueError("mean and rstd must be contiguous fp32 tensors of a value a row on the device of x")
+
+
+def clear_layer_norm_fwd(x, y, weight=None, bias=None, mean=None, rstd=None, weight_offset=0.0, eps=1e-6, stream=None):
+    """Layer normalisation of the rows of ``x`` ([N, C] or [B, N, C], bf16 or fp32, contiguous channels) into ``y`` (may be ``x``):
+    (x - mean) * rstd * (weight_offset + weight) + bias, with weight and bias [C], or [B, C] for a pair a batch entry (a modulated
+    layer: ``weight`` the scale, ``weight_offset`` 1, ``bias`` the shift).  ``mean``, ``rstd``: fp32, written for the backward pass."""
+    import torch
+    (B, N, C), strides = _norm_rows(x, y)
+    kind, wb = _norm_params(x, B, C, weight, bias)
+    _norm_stats(x, B, N, mean, rstd)
+    _on_device_of(x, stream, lambda st: _check(load().clear_layer_norm_fwd(
+        x.data_ptr(), y.data_ptr(), _ptr(weight), _ptr(bias), _ptr(mean), _ptr(rstd), B, N, C,
+        BF16 if x.dtype == torch.bfloat16 else F32, kind, *strides, *wb, weight_offset, eps, st), "clear_layer_norm_fwd"))
+    return y
+
+
+def clear_layer_norm_bwd(x, dy, weight, mean, rstd, dx, dweight=None, dbias=None, weight_offset=0.0, stream=None):
+    """Gradient of ``clear_layer_norm_fwd`` from its input, its statistics and the gradient ``dy`` of its output: ``dx`` (may be ``x``
+    or ``dy``) and, where given, ``dweight`` and ``dbias``, summed over all rows ([C]) or those of each batch entry ([B, C], as the
+    weight is).  Returns the three."""
+    import torch
+    (B, N, C), strides = _norm_rows(x, dy, dx)
+    kind, sums = _norm_params(x, B, C, weight, dweight, dbias)
+    _norm_stats(x, B, N, mean, rstd)
+    forms = {p.dim() for p in (weight, dweight, dbias) if p is not None}
+    if len(forms) > 1:
+        raise ValueError("weight, dweight and dbias must all be [C] or all be [B, C]")
+    per_batch = 1 if forms == {2} else 0
+    device = x.device
+
+    def call(st):
+        n_bytes = 0 if dweight is None and dbias is None else _workspace_bytes("clear_layer_norm_bwd_workspace", device.index, B, N, C,
+                                                                              per_batch)
+        ws = _workspace(n_bytes, device, st) if n_bytes else None
+        _check(load().clear_layer_norm_bwd(
+            x.data_ptr(), dy.data_ptr(), _ptr(weight), mean.data_ptr(), rstd.data_ptr(), dx.data_ptr(), _ptr(dweight), _ptr(dbias),
+            B, N, C, BF16 if x.dtype == torch.bfloat16 else F32, kind, per_batch, *strides, *sums, weight_offset, _ptr(ws), n_bytes,
+            st), "clear_layer_norm_bwd")
+
+    _on_device_of(x, stream, call)
+    return dx, dweight, dbias
 
 
 def clear_log_scale_factor(n_tokens: int, n_train_tokens: int) -> float:

@@ -118,6 +118,50 @@ int launch_text_merge(const float *records, int n_parts, int n_bh, int n_text, i
 int launch_qk_prep(const void *q_in, const void *k_in, void *q_out, void *k_out, const float *gain_q, const float *gain_k,
                    int n_bh, int grid_h, int grid_w, int n_text, int head_dim, int dtype, const int axes_dim[3],
                    double theta, double ntk_factor, float eps, float q_factor, cudaStream_t stream);
+// Its gradient, with the sums of the gains' gradients (`workspace`: prep_bwd_workspace bytes, not read where neither is wanted).
+int prep_bwd_workspace(int head_dim, size_t *bytes);
+int launch_prep_bwd(const void *q, const void *k, const void *dq_rot, const void *dk_rot, void *dq, void *dk, const float *gain_q,
+                    const float *gain_k, float *dgain_q, float *dgain_k, int n_bh, int grid_h, int grid_w, int n_text, int head_dim,
+                    int dtype, const int axes_dim[3], double theta, double ntk_factor, float eps, float q_factor, void *workspace,
+                    cudaStream_t stream);
+
+// Rotary positions of one or two tensors (the second one's `in` may be null), strides in elements.
+constexpr int kMaxRopePairs = 128;
+struct RopeIo {
+    const void *in;
+    void *out;
+    int heads;
+    long long in_stride_b, in_stride_h, in_stride_n, out_stride_b, out_stride_h, out_stride_n;
+};
+struct RopeArgs {
+    RopeIo io[2];
+    const void *positions;
+    long long pos_stride_b, pos_stride_n;
+    int pos64;
+    const double *frequencies;
+    const int *axes_dim;
+    int n_axes, B, N, head_dim, dtype, half, inverse;
+    float factor;
+};
+int launch_rope(const RopeArgs &a, cudaStream_t stream);
+
+// Layer norm of [B, N, C] rows; pointers of the other direction are null.  Strides in elements.
+struct NormArgs {
+    const void *x, *dy;
+    void *out;
+    const void *weight, *bias;
+    void *dweight, *dbias;
+    const float *mean_in, *rstd_in;
+    float *mean, *rstd;
+    int B, N, C, dtype, param_dtype, per_batch;
+    long long x_stride_b, x_stride_n, dy_stride_b, dy_stride_n, out_stride_b, out_stride_n;
+    long long w_stride_b, bias_stride_b, dw_stride_b, db_stride_b;
+    float offset, eps;
+    void *workspace;
+};
+int norm_bwd_workspace(int B, int N, int C, int per_batch, size_t *bytes);
+int launch_norm_fwd(const NormArgs &a, cudaStream_t stream);
+int launch_norm_bwd(const NormArgs &a, cudaStream_t stream);
 // Backward pass on the tensor cores (bf16): a query-role and a key-role launch over the plan's tile schedule (a plan made
 // with Shape::backward).
 int launch_bwd_tc(const clear_plan &p, const void *q, const void *k, const void *v, const void *d_out, void *dq, void *dk,

@@ -1,0 +1,722 @@
+"""GPU parity of layer norm, rotary positions and the gradient of the Q/K preparation, through the binding, against the fp64 oracle.
+
+Bounds.  u = 2^-24 is half a step of fp32 and 2^-8 one of bf16, both relative: a result that is stored as bf16 is off by 2^-8 of itself
+on top of what fp32 arithmetic does.  A sum of fp32 values is off by at most (longest chain of additions) * u * (sum of magnitudes).
+"""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from oracle import clear_oracle_layer as oracle
+from oracle import clear_oracle_qk_prep as oracle_prep
+from paper_2412_16112_b200 import binding as clear
+
+pytestmark = pytest.mark.gpu
+U = 2.0 ** -24
+DTYPES = {"bf16": torch.bfloat16, "f32": torch.float32}
+
+
+def _np(t):
+    return t.detach().cpu().to(torch.float64).numpy()
+
+
+def _close(got, want, slack, dtype):
+    """|got - want| within the arithmetic's slack plus the rounding of the result when it is stored."""
+    got = _np(got)
+    assert np.isfinite(got).all()
+    step = 2.0 ** -8 if dtype == torch.bfloat16 else U
+    excess = np.abs(got - want) - (slack + step * (np.abs(want) + slack))
+    assert excess.max() <= 0, (float(np.abs(got - want).max()), float(excess.max()), np.unravel_index(excess.argmax(), excess.shape))
+
+
+def _randn(shape, seed, dtype=torch.float32, device="cuda"):
+    g = torch.Generator().manual_seed(seed)
+    return torch.randn(*shape, generator=g).to(dtype).to(device)
+
+
+# ---- layer norm ------------------------------------------------------------------------------------------------------
+
+
+def _chain(C):
+    """Longest chain of additions of a row's sum: a thread's channels (16 at most in the tile kernels' backward, 128 forward, C / 256
+    beyond), then the levels of the lanes and warps."""
+    return max(128, -(-C // 256)) + 32
+
+
+def _norm_bound(x, w, offset, mean, rstd, C):
+    k = _chain(C) * U
+    r = rstd[..., None]
+    h = np.abs(x - mean[..., None]) * r
+    gain = np.abs(oracle._gain(w, offset)) + 2 * U
+    # the mean is off by k of the mean magnitude, the variance by 2 k of itself (and the square of the mean's error), so rstd by k
+    return gain * (k * np.abs(x).mean(-1, keepdims=True) * r * (1 + h) + h * (2 * k + 8 * U)) + 4 * U * gain * h
+
+
+def _norm_inputs(B, N, C, dtype, pdtype, form, seed, device="cuda"):
+    x = (_randn((B, N, C), seed) * 1.5 + 3.0 * _randn((C,), seed + 1)).to(dtype)
+    dy = _randn((B, N, C), seed + 2, dtype)
+    shape = (B, C) if form == "batch" else (C,)
+    w, b = (None, None) if form == "none" else (0.5 * _randn(shape, seed + 3, torch.float32).to(pdtype),
+                                                _randn(shape, seed + 4, torch.float32).to(pdtype))
+    return x, dy, w, b
+
+
+def _check_norm(x, dy, w, b, offset, eps=1e-5, y=None, dx=None, dw=None, db=None, sums=True):
+    B, N, C = x.shape
+    dev = x.device
+    mean, rstd = (torch.full((B, N), float("nan"), device=dev) for _ in range(2))
+    y = torch.full_like(x, float("nan")) if y is None else y
+    xn, dyn, wn = _np(x), _np(dy), None if w is None else _np(w)
+    want, m, r = oracle.layer_norm(xn, wn, None if b is None else _np(b), offset, eps)
+    clear.clear_layer_norm_fwd(x, y, w, b, mean, rstd, weight_offset=offset, eps=eps)
+    bias = 0 if b is None else 2 * U * np.abs(oracle._rows(_np(b)))
+    _close(y, want, _norm_bound(xn, wn, offset, m, r, C) + bias + 1e-30, x.dtype)
+    k = _chain(C) * U
+    _close(mean, m, k * np.abs(xn).mean(-1), torch.float32)
+    _close(rstd, r, r * (2 * k + 4 * U), torch.float32)
+    # the gradient is that of the given statistics
+    mn, rn = _np(mean), _np(rstd)
+    per_batch = w is not None and w.dim() == 2
+    shape = (B, C) if per_batch else (C,)
+    kind = x.dtype if w is None else w.dtype
+    dx = torch.full_like(x, float("nan")) if dx is None else dx
+    if sums:
+        dw = torch.full(shape, float("nan"), device=dev, dtype=kind) if dw is None else dw
+        db = torch.full(shape, float("nan"), device=dev, dtype=kind) if db is None else db
+    wdx, wdw, wdb = oracle.layer_norm_grad(xn, dyn, wn, mn, rn, offset, per_batch)
+    clear.clear_layer_norm_bwd(x, dy, w, mean, rstd, dx, dw, db, weight_offset=offset)
+    h = np.abs(xn - mn[..., None]) * rn[..., None]
+    g = np.abs(dyn * oracle._gain(wn, offset))
+    kb = k + 10 * U
+    rows = rn[..., None] * (kb * g.mean(-1, keepdims=True) + h * kb * (g * h).mean(-1, keepdims=True)
+                            + 10 * U * (g + g.mean(-1, keepdims=True) + h * (g * h).mean(-1, keepdims=True)))
+    _close(dx, wdx, rows + 1e-30, x.dtype)
+    if sums:
+        over = 1 if per_batch else (0, 1)
+        n = (N if per_batch else B * N) + 16
+        _close(dw, wdw, (n + 4) * U * (np.abs(dyn) * h).sum(over), kind)
+        _close(db, wdb, n * U * np.abs(dyn).sum(over), kind)
+
+
+@pytest.mark.parametrize("dtype,pdtype", [("bf16", "bf16"), ("bf16", "f32"), ("f32", "f32")])
+@pytest.mark.parametrize("C", [1, 2, 7, 8, 31, 33, 64, 100, 255, 256, 264, 768, 1003, 1024, 1536, 2048, 4096, 8192, 8200])
+@pytest.mark.parametrize("form", ["shared", "batch"])
+def test_layer_norm_widths(dtype, pdtype, C, form):
+    x, dy, w, b = _norm_inputs(2, 5, C, DTYPES[dtype], DTYPES[pdtype], form, C)
+    _check_norm(x, dy, w, b, 1.0)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("C", [20000, 32768, 32776, 33001])
+def test_layer_norm_of_very_long_rows(dtype, C):
+    x, dy, w, b = _norm_inputs(1, 3, C, DTYPES[dtype], DTYPES[dtype], "shared", C)
+    _check_norm(x, dy, w, b, 0.0)
+
+
+@pytest.mark.parametrize("B,N", [(1, 1), (1, 2), (3, 1), (1, 37), (2, 300), (5, 61), (300, 2), (1, 5000), (3, 1237)])
+@pytest.mark.parametrize("dtype,C", [("bf16", 96), ("bf16", 50), ("f32", 61), ("f32", 520)])
+@pytest.mark.parametrize("form", ["none", "shared", "batch"])
+def test_layer_norm_rows(B, N, dtype, C, form):
+    x, dy, w, b = _norm_inputs(B, N, C, DTYPES[dtype], torch.float32, form, B * 1000 + N)
+    _check_norm(x, dy, w, b, 0.5)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("C", [64, 1536, 9000])
+def test_layer_norm_strides_and_alignment(dtype, C):
+    t = DTYPES[dtype]
+    B, N = 2, 9
+    x, dy, w, b = _norm_inputs(B, N, C, t, t, "batch", 7)
+    # channels of a wider row, tokens of a longer sequence, rows in reverse order, at every offset from the boundary
+    for pad, lead in ((0, 0), (8, 8), (5, 1), (3, 2)):
+        def wide(src):
+            out = torch.full((B, N + 3, C + pad + lead), 7.0, device="cuda", dtype=t)
+            view = out[:, 1:N + 1, lead:lead + C]
+            view.copy_(src)
+            return out, view
+        (_, xv), (_, dyv), (yb, yv), (dxb, dxv) = wide(x), wide(dy), wide(x), wide(x)
+        mod = torch.full((B, 3 * C + pad), 7.0, device="cuda", dtype=t)
+        wv, bv = mod[:, C:2 * C], mod[:, 2 * C:3 * C]
+        wv.copy_(w)
+        bv.copy_(b)
+        grads = torch.full((B, 2 * C + pad), 7.0, device="cuda", dtype=t)
+        _check_norm(xv, dyv, wv, bv, 1.0, y=yv, dx=dxv, dw=grads[:, :C], db=grads[:, C:2 * C])
+        for whole, view in ((yb, yv), (dxb, dxv)):   # nothing beside the rows is written
+            view.fill_(7.0)
+            assert bool((whole == 7.0).all())
+        assert bool((grads[:, 2 * C:] == 7.0).all())
+    # rows far apart in an order of their own: tokens before batch entries
+    xt = x.transpose(0, 1).contiguous().transpose(0, 1)
+    dyt = dy.transpose(0, 1).contiguous().transpose(0, 1)
+    _check_norm(xt, dyt, w, b, 1.0, y=torch.empty_like(xt), dx=torch.empty_like(xt))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("C", [96, 61, 1536, 20001])
+def test_layer_norm_in_place(dtype, C):
+    x, dy, w, b = _norm_inputs(2, 11, C, DTYPES[dtype], torch.float32, "shared", 5)
+    mean, rstd = (torch.empty(2, 11, device="cuda") for _ in range(2))
+    y = clear.clear_layer_norm_fwd(x, torch.empty_like(x), w, b, mean, rstd)
+    assert torch.equal(clear.clear_layer_norm_fwd(x.clone(), x.clone(), w, b), y)
+    own = x.clone()
+    assert torch.equal(clear.clear_layer_norm_fwd(own, own, w, b), y)
+    dw, db = torch.empty(C, device="cuda"), torch.empty(C, device="cuda")
+    want = [t.clone() for t in clear.clear_layer_norm_bwd(x, dy, w, mean, rstd, torch.empty_like(x), dw, db)]
+    for over in ("x", "dy"):
+        xc, dyc = x.clone(), dy.clone()
+        got = clear.clear_layer_norm_bwd(xc, dyc, w, mean, rstd, xc if over == "x" else dyc, dw, db)
+        for a, e in zip(got, want):
+            assert torch.equal(a, e), over
+
+
+def test_layer_norm_optional_parts():
+    x, dy, w, b = _norm_inputs(2, 40, 200, torch.bfloat16, torch.float32, "shared", 9)
+    _check_norm(x, dy, w, None, 0.0)
+    _check_norm(x, dy, None, None, 3.0)      # without a weight the offset counts for nothing
+    _check_norm(x, dy, w, b, 0.0, sums=False)
+    mean, rstd = x.float().mean(-1), torch.rsqrt(x.float().var(-1, correction=0) + 1e-5)
+    dw, db = torch.empty(200, device="cuda"), torch.empty(200, device="cuda")
+    both = [t.clone() for t in clear.clear_layer_norm_bwd(x, dy, w, mean, rstd, torch.empty_like(x), dw, db)]
+    only = clear.clear_layer_norm_bwd(x, dy, w, mean, rstd, torch.empty_like(x), dweight=torch.empty_like(dw))
+    assert torch.equal(only[0], both[0]) and torch.equal(only[1], both[1]) and only[2] is None
+    only = clear.clear_layer_norm_bwd(x, dy, w, mean, rstd, torch.empty_like(x), dbias=torch.empty_like(dw))
+    assert torch.equal(only[2], both[2]) and only[1] is None
+    # [N, C] is a batch of one
+    flat = [t.clone() for t in clear.clear_layer_norm_bwd(x[0], dy[0], w, mean[0].contiguous(), rstd[0].contiguous(),
+                                                          torch.empty_like(x[0]), dw, db)]
+    one = clear.clear_layer_norm_bwd(x[:1], dy[:1], w, mean[:1], rstd[:1], torch.empty_like(x[:1]), dw, db)
+    assert torch.equal(flat[0], one[0][0]) and torch.equal(flat[1], one[1])
+
+
+def test_layer_norm_without_rows():
+    x = torch.empty(2, 0, 24, device="cuda")
+    stats = torch.empty(2, 0, device="cuda")
+    clear.clear_layer_norm_fwd(x, torch.empty_like(x))
+    for shape in ((24,), (2, 24)):
+        w, dw, db = torch.ones(shape, device="cuda"), torch.full(shape, 7.0, device="cuda"), torch.full(shape, 7.0, device="cuda")
+        clear.clear_layer_norm_bwd(x, x, w, stats, stats, torch.empty_like(x), dw, db)
+        assert not dw.any() and not db.any()
+
+
+def test_layer_norm_statistics_of_rows_far_from_zero():
+    """An offset common to a row costs no accuracy: 1000 + N(0, 1) in fp32 (the inputs' own rounding is in the oracle's too)."""
+    x = 1000.0 + _randn((1, 64, 1024), 1)
+    _check_norm(x, _randn((1, 64, 1024), 2), None, None, 0.0)
+    const = torch.full((1, 3, 512), 5.0, device="cuda")
+    y = clear.clear_layer_norm_fwd(const, torch.empty_like(const))
+    assert not y.any()
+
+
+@pytest.mark.parametrize("C", [512, 61, 6000])
+def test_layer_norm_rows_that_are_not_finite_stay_alone(C):
+    x, dy, w, b = _norm_inputs(1, 40, C, torch.float32, torch.float32, "shared", 21)
+    clean = clear.clear_layer_norm_fwd(x, torch.empty_like(x), w, b)
+    bad = x.clone()
+    bad[0, 3, C // 2], bad[0, 17, 0], bad[0, 39, C - 1] = float("nan"), float("inf"), -float("inf")
+    mean, rstd = (torch.empty(1, 40, device="cuda") for _ in range(2))
+    y = clear.clear_layer_norm_fwd(bad, torch.empty_like(x), w, b, mean, rstd)
+    rows = [3, 17, 39]
+    fine = [i for i in range(40) if i not in rows]
+    assert torch.equal(y[0, fine], clean[0, fine]) and bool(torch.isnan(y[0, rows]).all())
+    dx = clear.clear_layer_norm_bwd(bad, dy, w, mean, rstd, torch.empty_like(x))[0]
+    assert bool(torch.isfinite(dx[0, fine]).all()) and bool(torch.isnan(dx[0, rows]).all())
+
+
+def test_layer_norm_sums_repeat_bit_for_bit():
+    x, dy, w, b = _norm_inputs(3, 2111, 768, torch.bfloat16, torch.bfloat16, "batch", 2)
+    mean, rstd = (torch.empty(3, 2111, device="cuda") for _ in range(2))
+    clear.clear_layer_norm_fwd(x, torch.empty_like(x), w, b, mean, rstd)
+    runs = []
+    for _ in range(3):
+        runs.append(clear.clear_layer_norm_bwd(x, dy, w, mean, rstd, torch.empty_like(x), torch.empty_like(w), torch.empty_like(w)))
+    for r in runs[1:]:
+        assert all(torch.equal(a, e) for a, e in zip(r, runs[0]))
+
+
+def test_layer_norm_offsets_beyond_32_bits():
+    """Rows 2^31 and more elements apart."""
+    C, far = 264, 2 ** 31 + 8
+    base = torch.zeros(far + 4 * C, device="cuda", dtype=torch.bfloat16)
+    src = _randn((2, 2, C), 3, torch.bfloat16)
+
+    def apart():
+        return base.as_strided((2, 2, C), (C, far, 1))
+
+    apart().copy_(src)
+    w = _randn((C,), 4)
+    y = clear.clear_layer_norm_fwd(apart(), torch.empty_like(src), w, None)
+    assert torch.equal(y, clear.clear_layer_norm_fwd(src, torch.empty_like(src), w, None))
+    clear.clear_layer_norm_fwd(src, apart(), w, None)
+    assert torch.equal(apart(), y)
+    mean, rstd = (torch.empty(2, 2, device="cuda") for _ in range(2))
+    clear.clear_layer_norm_fwd(src, torch.empty_like(src), w, None, mean, rstd)
+    apart().copy_(src)
+    dy = _randn((2, 2, C), 5, torch.bfloat16)
+    want = clear.clear_layer_norm_bwd(src, dy, w, mean, rstd, torch.empty_like(src), torch.empty_like(w))
+    got = clear.clear_layer_norm_bwd(apart(), dy, w, mean, rstd, apart(), torch.empty_like(w))
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+
+
+def test_layer_norm_gradient_against_differences():
+    """<dx, v> of the kernels against (f(x + t v) - f(x - t v)) / 2t of the kernel's own forward, f = sum(y dy) in 64 bits."""
+    x, dy, w, b = _norm_inputs(1, 8, 333, torch.float32, torch.float32, "shared", 31)
+    mean, rstd = (torch.empty(1, 8, device="cuda") for _ in range(2))
+    clear.clear_layer_norm_fwd(x, torch.empty_like(x), w, b, mean, rstd, weight_offset=1.0, eps=1e-3)
+    dx, dw, db = clear.clear_layer_norm_bwd(x, dy, w, mean, rstd, torch.empty_like(x), torch.empty_like(w), torch.empty_like(b), 1.0)
+    v, vw = _randn(tuple(x.shape), 6), _randn((333,), 7)
+    t = 2.0 ** -7
+
+    def f(s):
+        y = clear.clear_layer_norm_fwd(x + s * v, torch.empty_like(x), w + s * vw, b, weight_offset=1.0, eps=1e-3)
+        return float((y.double() * dy.double()).sum())
+
+    slope = (f(t) - f(-t)) / (2 * t)
+    want = float((dx.double() * v.double()).sum() + (dw.double() * vw.double()).sum())
+    # truncation: t^2 / 6 times a third derivative, whose terms are dy h-like values of order one (rows are of scale 3: each order
+    # divides by it): 1e-5 * n^1/2 * 6; rounding: 4 fp32 steps a value of y, random, over t
+    n = x.numel()
+    assert abs(slope - want) <= math.sqrt(n) * (t * t * 6 + 4 * U * 10 / t)
+
+
+# ---- rotary positions ------------------------------------------------------------------------------------------------
+
+
+def _check_rope(q, k, positions, freqs, axes, layout, factor, q_out=None, k_out=None):
+    half = layout == clear.ROPE_HALF
+    pn, fn = positions.cpu().numpy(), freqs.numpy()
+    rot = sum(axes)
+    for call, inverse in ((clear.clear_rope_fwd, False), (clear.clear_rope_bwd, True)):
+        qo = torch.full_like(q, float("nan")) if q_out is None else q_out
+        ko = k_out if k_out is not None or k is None else torch.full_like(k, float("nan"))
+        call(q, k, qo, ko, positions, freqs, axes, layout, factor)
+        for x, out in ((q, qo),) if k is None else ((q, qo), (k, ko)):
+            xn = _np(x)
+            want = oracle.rotate(xn, pn, fn, axes, half, factor, inverse)
+            pairs = rot // 2
+            lo, hi = (slice(0, pairs), slice(pairs, rot)) if half else (slice(0, rot, 2), slice(1, rot, 2))
+            slack = np.zeros_like(xn)
+            # sine and cosine off by 4 steps (the angle by one), the products and their sum by 4 more, of the pair's length
+            slack[..., lo] = slack[..., hi] = np.hypot(xn[..., lo], xn[..., hi]) * abs(factor) * 10 * U
+            # positions beyond 2^20: the oracle's own angle, position * frequency in 64 bits, is off by 2^-53 of itself
+            slack += np.abs(pn).max() * np.abs(fn).max() * 2.0 ** -52 * (slack > 0) * (np.abs(xn).max() + 1) * abs(factor)
+            _close(out, want, slack, x.dtype)
+            assert (_np(out)[..., rot:] == xn[..., rot:]).all()   # the rest is copied, bit for bit
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("layout", [clear.ROPE_INTERLEAVED, clear.ROPE_HALF])
+@pytest.mark.parametrize("d,axes", [(128, (128,)), (128, (16, 56, 56)), (128, (64,)), (64, (8, 28, 28)), (64, (0, 0, 64)), (80, (40,)),
+                                    (80, (20,)), (72, (18,)), (40, (10,)), (2, (2,)), (7, (4,)), (33, (32,)), (256, (256,)),
+                                    (96, (24,)), (256, (2, 2, 2, 2, 2, 2, 2, 2))])
+def test_rope_heads(dtype, layout, d, axes):
+    B, H, Hk, N = 2, 5, 2, 7
+    q, k = _randn((B, H, N, d), d, DTYPES[dtype]), _randn((B, Hk, N, d), d + 1, DTYPES[dtype])
+    g = torch.Generator().manual_seed(d)
+    positions = torch.randint(-500, 5000, (B, N, len(axes)), generator=g, dtype=torch.int32).cuda()
+    freqs = torch.cat([clear.clear_rope_frequencies(a) for a in axes if a])
+    _check_rope(q, k, positions, freqs, axes, layout, 1.25)
+
+
+@pytest.mark.parametrize("B,H,Hk,N", [(1, 1, 0, 1), (2, 24, 8, 1), (1, 3, 3, 2), (1, 24, 24, 33), (3, 1, 1, 257), (1, 2, 1, 5000),
+                                      (1, 9, 1, 700)])
+@pytest.mark.parametrize("dtype,layout", [("bf16", clear.ROPE_HALF), ("f32", clear.ROPE_INTERLEAVED)])
+def test_rope_lengths(B, H, Hk, N, dtype, layout):
+    q = _randn((B, H, N, 64), N, DTYPES[dtype])
+    k = _randn((B, Hk, N, 64), N + 1, DTYPES[dtype]) if Hk else None
+    positions = torch.arange(N, device="cuda").reshape(1, N, 1)       # int64, shared by the batch entries
+    freqs = clear.clear_rope_frequencies(48, 1000.0, clear.ROPE_SCALE_PARTS, 4.0, 512.0)
+    _check_rope(q, k, positions, freqs, (48,), layout, 1.1)
+
+
+@pytest.mark.parametrize("bits", [32, 64])
+def test_rope_far_positions(bits):
+    """Positions to 2^31 and, in 64 bits, 2^40: the angles are as exact as near zero."""
+    top = 2 ** 31 - 1 if bits == 32 else 2 ** 40 + 12345
+    at = [0, 1, -1, 2 ** 20 + 1, 2 ** 24 + 1, -(2 ** 30) - 7, top, -top]
+    positions = torch.tensor(at, dtype=torch.int32 if bits == 32 else torch.int64, device="cuda").reshape(1, -1, 1)
+    q = _randn((1, 2, len(at), 16), 1)
+    freqs = torch.tensor([1.0, 0.5, 2.0 ** -10, 2.0 ** -20, 1e-4, 3.0, 2.0 * math.pi, 100.0], dtype=torch.float64)
+    got = _np(clear.clear_rope_fwd(q, None, torch.empty_like(q), None, positions, freqs, (16,), clear.ROPE_HALF))
+    # in 80-bit arithmetic: position times frequency is exact to 2^-64 of itself, 2^-18 rad at 2^47
+    turns = np.array(at, dtype=np.longdouble)[:, None] * (freqs.numpy().astype(np.longdouble) / (2 * np.longdouble(np.pi) + np.longdouble(2.4492935982947064e-16)))
+    t = ((turns - np.floor(turns)) * 2 * np.longdouble(np.pi)).astype(np.float64)[None, None]
+    x = _np(q)
+    want = np.concatenate([x[..., :8] * np.cos(t) - x[..., 8:] * np.sin(t), x[..., :8] * np.sin(t) + x[..., 8:] * np.cos(t)], -1)
+    err = np.abs(got - want) / np.tile(np.hypot(x[..., :8], x[..., 8:]), 2)
+    lost = np.tile(np.abs(turns).astype(np.float64) * 2 * math.pi * 2.0 ** -62, 2)[None, None]
+    assert (err <= 10 * U + lost).all(), float(err.max())
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("layout", [clear.ROPE_INTERLEAVED, clear.ROPE_HALF])
+@pytest.mark.parametrize("lead", [0, 1, 2, 4])
+def test_rope_strides(dtype, layout, lead):
+    """Out of a packed projection (at any offset from the boundary) head by head and back; what lies beside is left alone."""
+    t = DTYPES[dtype]
+    B, N, H, Hk, d, axes = 2, 19, 6, 2, 64, (32,)
+    flat = _randn((B, N, (H + 2 * Hk) * d + lead), 3, t)
+    rows = flat[..., lead:].unflatten(-1, (H + 2 * Hk, d))
+    q, k = rows[:, :, :H].transpose(1, 2), rows[:, :, H:H + Hk].transpose(1, 2)
+    positions = torch.randint(0, 100, (B, N, 1), dtype=torch.int32, generator=torch.Generator().manual_seed(1)).cuda()
+    freqs = clear.clear_rope_frequencies(32)
+    _check_rope(q, k, positions, freqs, axes, layout, 1.0)
+    heads = [torch.empty(B, H, N, d, device="cuda", dtype=t), torch.empty(B, Hk, N, d, device="cuda", dtype=t)]
+    clear.clear_rope_fwd(q, k, *heads, positions, freqs, axes, layout)
+    # back into a packed tensor
+    out = torch.full_like(flat, 7.0)
+    view = out[..., lead:].unflatten(-1, (H + 2 * Hk, d))
+    clear.clear_rope_fwd(q, k, view[:, :, :H].transpose(1, 2), view[:, :, H:H + Hk].transpose(1, 2), positions, freqs, axes, layout)
+    assert torch.equal(view[:, :, :H].transpose(1, 2), heads[0]) and torch.equal(view[:, :, H:H + Hk].transpose(1, 2), heads[1])
+    assert bool((view[:, :, H + Hk:] == 7.0).all()) and bool((out[..., :lead] == 7.0).all())
+    # in place, in the packed tensor
+    values = rows[:, :, H + Hk:].clone()
+    clear.clear_rope_fwd(q, k, q, k, positions, freqs, axes, layout)
+    assert torch.equal(q, heads[0]) and torch.equal(k, heads[1]) and torch.equal(rows[:, :, H + Hk:], values)
+
+
+def test_rope_one_in_place_and_one_not():
+    q, k = _randn((1, 4, 30, 48), 1), _randn((1, 2, 30, 48), 2)
+    positions, freqs = torch.arange(30, device="cuda").reshape(1, 30, 1), clear.clear_rope_frequencies(16)
+    want = clear.clear_rope_fwd(q, k, torch.empty_like(q), torch.empty_like(k), positions, freqs, (16,))
+    q2, k2 = q.clone(), torch.full_like(k, float("nan"))
+    clear.clear_rope_fwd(q2, k, q2, k2, positions, freqs, (16,))
+    assert torch.equal(q2, want[0]) and torch.equal(k2, want[1])
+
+
+def test_rope_reads_heads_that_share_memory():
+    """An input may be expanded: one row of keys read for all heads."""
+    k = _randn((1, 1, 9, 32), 1).expand(1, 4, 9, 32)
+    positions, freqs = torch.arange(9, device="cuda").reshape(1, 9, 1), clear.clear_rope_frequencies(32)
+    got = clear.clear_rope_fwd(k, None, torch.empty(1, 4, 9, 32, device="cuda"), None, positions, freqs, (32,))
+    assert torch.equal(got, clear.clear_rope_fwd(k.contiguous(), None, torch.empty(1, 4, 9, 32, device="cuda"), None, positions, freqs,
+                                                 (32,)))
+
+
+def test_rope_offsets_beyond_32_bits():
+    far = 2 ** 31 + 16
+    base = torch.zeros(far + 4096, device="cuda", dtype=torch.bfloat16)
+    src = _randn((1, 2, 5, 64), 1, torch.bfloat16)
+    apart = base.as_strided((1, 2, 5, 64), (0, far, 64, 1))
+    apart.copy_(src)
+    positions, freqs = torch.arange(5, device="cuda").reshape(1, 5, 1), clear.clear_rope_frequencies(64)
+    want = clear.clear_rope_fwd(src, None, torch.empty_like(src), None, positions, freqs, (64,))
+    assert torch.equal(clear.clear_rope_fwd(apart, None, torch.empty_like(src), None, positions, freqs, (64,)), want)
+    clear.clear_rope_fwd(apart, None, apart, None, positions, freqs, (64,))
+    assert torch.equal(apart, want)
+
+
+def test_rope_special_values_and_nothing_to_do():
+    q = _randn((1, 1, 4, 8), 1)
+    q[0, 0, 1, 0], q[0, 0, 2, 7] = float("nan"), float("inf")
+    positions, freqs = torch.arange(4, device="cuda").reshape(1, 4, 1), clear.clear_rope_frequencies(4)
+    got = clear.clear_rope_fwd(q, None, torch.empty_like(q), None, positions, freqs, (4,))
+    assert torch.isnan(got[0, 0, 1, :2]).all() and torch.isfinite(got[0, 0, 1, 2:]).all() and torch.isinf(got[0, 0, 2, 7])
+    assert torch.isfinite(got[0, 0, [0, 3]]).all()
+    empty = torch.empty(2, 3, 0, 8, device="cuda")
+    clear.clear_rope_fwd(empty, None, empty, None, torch.empty(2, 0, 1, device="cuda", dtype=torch.int32), freqs, (4,))
+
+
+def test_rope_gradient_is_the_transpose():
+    """<R x, y> = <x, R^T y> for the kernels themselves: both sides are sums of n products, each off by 12 steps."""
+    x, y = _randn((2, 3, 50, 64), 1), _randn((2, 3, 50, 64), 2)
+    positions = torch.randint(0, 10 ** 6, (2, 50, 2), dtype=torch.int32, generator=torch.Generator().manual_seed(2)).cuda()
+    freqs = torch.cat([clear.clear_rope_frequencies(24), clear.clear_rope_frequencies(16)])
+    for layout in (clear.ROPE_INTERLEAVED, clear.ROPE_HALF):
+        a = clear.clear_rope_fwd(x, None, torch.empty_like(x), None, positions, freqs, (24, 16), layout, 1.3).double()
+        b = clear.clear_rope_bwd(y, None, torch.empty_like(y), None, positions, freqs, (24, 16), layout, 1.3).double()
+        assert abs(float((a * y.double()).sum() - (x.double() * b).sum())) <= 24 * U * float((a.norm() * y.double().norm()))
+
+
+# ---- gradient of the Q/K preparation ---------------------------------------------------------------------------------
+
+
+def _check_prep(B, H, gh, gw, T, d, axes, dtype, gains, ntk, qf, over=None, eps=1e-6):
+    N = T + gh * gw
+    q, k, dqr, dkr = (2.0 * _randn((B, H, N, d), 10 * N + i, DTYPES[dtype]) for i in range(4))
+    gq, gk = ((1.0 + 0.2 * _randn((d,), d + i)) if gains else None for i in range(2))
+    dgq, dgk = (torch.full((d,), float("nan"), device="cuda") for _ in range(2))
+    dq = {None: lambda: torch.full_like(q, float("nan")), "x": q.clone, "dy": dqr.clone}[over]()
+    dk = {None: lambda: torch.full_like(q, float("nan")), "x": k.clone, "dy": dkr.clone}[over]()
+    q_in, k_in = (dq, dk) if over == "x" else (q, k)
+    dq_in, dk_in = (dq, dk) if over == "dy" else (dqr, dkr)
+    clear.clear_qk_norm_rope_bwd(q_in, k_in, dq_in, dk_in, dq, dk, gh, gw, T, axes, gq, gk, dgq, dgk, 10000.0, ntk, eps, qf)
+    pos = oracle_prep.token_positions(gh, gw, T)
+    for x, dy, got, gain, dgain, f in ((q, dqr, dq, gq, dgq, qf), (k, dkr, dk, gk, dgk, 1.0)):
+        xn, dyn = _np(x), _np(dy)
+        gn = None if gain is None else _np(gain)
+        want, wgain = oracle.qk_prep_grad(xn, dyn, gn, pos, axes, 10000.0, ntk, eps, f)
+        # u is off by 12 steps of its pair's length, the row's two sums by 13 + 12 of their magnitudes, everything else by a few
+        length = np.repeat(np.hypot(dyn[..., 0::2], dyn[..., 1::2]), 2, -1) * abs(f)
+        g = 1.0 if gn is None else np.abs(gn)
+        inv = 1 / np.sqrt((xn ** 2).mean(-1, keepdims=True) + eps)
+        along = (length * g * np.abs(xn)).mean(-1, keepdims=True)
+        slack = inv * (length * g + np.abs(xn) * inv ** 2 * along) * 40 * U
+        _close(got, want, slack, x.dtype)
+        rows = B * H * N
+        _close(dgain, wgain, (rows + 40) * U * (length * np.abs(xn) * inv).reshape(-1, d).sum(0), torch.float32)
+
+
+@pytest.mark.parametrize("B,H,gh,gw,T,d,axes,dtype,gains,ntk,qf", [
+    (1, 2, 16, 16, 16, 64, (8, 28, 28), "f32", True, 1.0, 1.0),      # the tiny fp32 configuration
+    (2, 3, 13, 19, 7, 128, (16, 56, 56), "bf16", True, 1.0, 1.0),
+    (2, 3, 13, 19, 7, 128, (16, 56, 56), "bf16", False, 10.0, 1.07),
+    (1, 5, 8, 16, 0, 128, (0, 64, 64), "f32", True, 10.0, 0.5),      # no text, heads that do not come in twos
+    (1, 1, 1, 1, 0, 64, (0, 0, 64), "bf16", True, 1.0, 1.0),         # a single row
+    (1, 1, 1, 70, 2, 64, (2, 2, 60), "bf16", True, 1.0, 1.0),
+    (2, 2, 33, 9, 130, 128, (128, 0, 0), "f32", False, 1.0, 1.0),    # nothing turns
+    (3, 7, 1, 1, 1, 128, (16, 56, 56), "f32", True, 2.0, 1.0),       # fewer tokens than warps
+    (1, 24, 24, 40, 5, 64, (0, 0, 64), "bf16", True, 2.0, 1.0),
+    (1, 2, 70, 70, 60, 128, (16, 56, 56), "bf16", True, 1.0, 1.0),   # more tokens than warps
+])
+def test_prep_gradient(B, H, gh, gw, T, d, axes, dtype, gains, ntk, qf):
+    for over in (None, "x", "dy"):
+        _check_prep(B, H, gh, gw, T, d, axes, dtype, gains, ntk, qf, over)
+
+
+def test_prep_gradient_without_sums_and_repeats():
+    N, d = 5 + 6 * 7, 64
+    q, k, dqr, dkr = (_randn((2, 3, N, d), i, torch.bfloat16) for i in range(4))
+    args = (6, 7, 5, (8, 28, 28))
+    gains = [1.0 + 0.2 * _randn((d,), 9), 1.0 + 0.2 * _randn((d,), 8)]
+
+    def new():
+        return torch.empty_like(q), torch.empty_like(q)
+
+    full = clear.clear_qk_norm_rope_bwd(q, k, dqr, dkr, *new(), *args, *gains, torch.empty(d, device="cuda"), torch.empty(d, device="cuda"))
+    again = clear.clear_qk_norm_rope_bwd(q, k, dqr, dkr, *new(), *args, *gains, torch.empty(d, device="cuda"), torch.empty(d, device="cuda"))
+    assert all(torch.equal(a, b) for a, b in zip(full, again))
+    none = clear.clear_qk_norm_rope_bwd(q, k, dqr, dkr, *new(), *args, *gains)
+    assert torch.equal(none[0], full[0]) and torch.equal(none[1], full[1]) and none[2] is None
+    one = clear.clear_qk_norm_rope_bwd(q, k, dqr, dkr, *new(), *args, *gains, dgain_k=torch.empty(d, device="cuda"))
+    assert torch.equal(one[3], full[3]) and one[2] is None
+
+
+def test_prep_gradient_of_zero_rows_and_rows_that_are_not_finite():
+    """A row of zeros has inv = 1 / sqrt(eps); a NaN or infinity reaches its own row (and the gains' sums), no other."""
+    q, k, dqr, dkr = (_randn((1, 2, 10, 64), i) for i in range(4))
+    q[0, 0, 3] = 0.0
+    args = (3, 3, 1, (8, 28, 28))
+    want = oracle.qk_prep_grad(_np(q), _np(dqr), None, oracle_prep.token_positions(3, 3, 1), args[3], 10000.0, 1.0, 1e-6, 1.0)[0]
+    dq, dk, _, _ = clear.clear_qk_norm_rope_bwd(q, k, dqr, dkr, torch.empty_like(q), torch.empty_like(q), *args)
+    np.testing.assert_allclose(_np(dq)[0, 0, 3], want[0, 0, 3], rtol=40 * U, atol=40 * U * 1000 * 4)
+    bad = q.clone()
+    bad[0, 1, 4, 5], bad[0, 0, 8, 0] = float("nan"), float("inf")
+    got = clear.clear_qk_norm_rope_bwd(bad, k, dqr, dkr, torch.empty_like(q), torch.empty_like(q), *args)
+    keep = torch.ones(1, 2, 10, dtype=torch.bool, device="cuda")
+    keep[0, 1, 4] = keep[0, 0, 8] = False
+    assert torch.equal(got[0][keep], dq[keep]) and torch.equal(got[1], dk) and not torch.isfinite(got[0][0, 1, 4]).any()
+
+
+def test_prep_gradient_against_differences():
+    """<dq, v> + <dgain, vg> against differences of clear_qk_norm_rope itself."""
+    q, k, dqr, dkr = (_randn((1, 2, 21, 64), i) for i in range(4))
+    gain, args = 1.0 + 0.2 * _randn((64,), 5), (4, 5, 1, (8, 28, 28))
+    dq, _, dg, _ = clear.clear_qk_norm_rope_bwd(q, k, dqr, dkr, torch.empty_like(q), torch.empty_like(q), *args, gain, None,
+                                                torch.empty(64, device="cuda"), None, eps=1e-3, q_factor=0.8)
+    v, vg = _randn(tuple(q.shape), 7), _randn((64,), 8)
+    t = 2.0 ** -7
+
+    def f(s):
+        out = clear.clear_qk_norm_rope(q + s * v, k, torch.empty_like(q), torch.empty_like(k), *args, gain + s * vg, None, eps=1e-3,
+                                       q_factor=0.8)[0]
+        return float((out.double() * dqr.double()).sum())
+
+    slope, want = (f(t) - f(-t)) / (2 * t), float((dq.double() * v.double()).sum() + (dg.double() * vg.double()).sum())
+    # truncation t^2 / 6 times third derivatives of order 6 a value; the forward kernel's angles are good to 1e-6 here, the same in
+    # both terms of the difference; rounding 4 steps of values up to 4, over t
+    assert abs(slope - want) <= math.sqrt(q.numel()) * (t * t * 6 + 4 * U * 4 / t) + 1e-5 * q.numel() ** 0.5 * 4
+
+
+# ---- streams, graphs, workspaces -------------------------------------------------------------------------------------
+
+
+def _all_calls(seed, n=700):
+    """Every operator on inputs of its own; returns a function that runs them all and the list of outputs."""
+    x, dy, w, b = _norm_inputs(2, n, 256, torch.bfloat16, torch.bfloat16, "batch", seed)
+    y, dx, dw, db = torch.empty_like(x), torch.empty_like(x), torch.empty_like(w), torch.empty_like(w)
+    mean, rstd = (torch.empty(2, n, device="cuda") for _ in range(2))
+    q, k, dqr, dkr = (_randn((1, 4, n, 64), seed + i, torch.bfloat16) for i in range(4))
+    qr, kr, qb, kb, dq, dk = (torch.empty_like(q) for _ in range(6))
+    dg = [torch.empty(64, device="cuda") for _ in range(2)]
+    gains = [1.0 + 0.2 * _randn((64,), seed + 9 + i) for i in range(2)]
+    positions, freqs = torch.arange(n, device="cuda").reshape(1, n, 1), clear.clear_rope_frequencies(64)
+
+    def go(stream=None):
+        clear.clear_layer_norm_fwd(x, y, w, b, mean, rstd, 1.0, stream=stream)
+        clear.clear_layer_norm_bwd(x, dy, w, mean, rstd, dx, dw, db, 1.0, stream=stream)
+        clear.clear_rope_fwd(q, k, qr, kr, positions, freqs, (64,), stream=stream)
+        clear.clear_rope_bwd(q, k, qb, kb, positions, freqs, (64,), stream=stream)
+        clear.clear_qk_norm_rope_bwd(q, k, dqr, dkr, dq, dk, n // 10, 10, n % 10, (8, 28, 28), *gains, *dg, stream=stream)
+
+    return go, [y, mean, rstd, dx, dw, db, qr, kr, qb, kb, dq, dk, *dg], [x, dy, q, k, dqr, dkr]
+
+
+def test_calls_on_streams_of_their_own():
+    jobs = [_all_calls(100 * i) for i in range(3)]
+    want = []
+    for go, outs, _ in jobs:
+        go()
+        torch.cuda.synchronize()
+        want.append([o.clone() for o in outs])
+        for o in outs:
+            o.fill_(float("nan"))
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in jobs]
+    for _ in range(4):
+        for (go, _, _), s in zip(jobs, streams):
+            go(stream=s)              # given explicitly
+        for (go, _, _), s in zip(jobs, streams):
+            with torch.cuda.stream(s):
+                go()                  # the current one
+    torch.cuda.synchronize()
+    for (_, outs, _), w in zip(jobs, want):
+        assert all(torch.equal(o, e) for o, e in zip(outs, w))
+
+
+def test_captured_calls_replay_on_new_inputs():
+    """Two graphs of the same calls, replayed side by side, each with workspaces of its own."""
+    jobs = [_all_calls(7), _all_calls(8)]
+    graphs = []
+    for go, _, _ in jobs:
+        go()
+        torch.cuda.synchronize()
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            go()
+        graphs.append(g)
+    streams = [torch.cuda.Stream() for _ in jobs]
+    for turn in range(2):
+        for _, outs, ins in jobs:
+            for t in ins:
+                t.copy_(t.roll(1, dims=-2) * 0.75)
+            for o in outs:
+                o.fill_(float("nan"))
+        torch.cuda.synchronize()
+        for g, s in zip(graphs, streams):
+            with torch.cuda.stream(s):
+                g.replay()
+        torch.cuda.synchronize()
+        for go, outs, _ in jobs:
+            got = [o.clone() for o in outs]
+            go()
+            torch.cuda.synchronize()
+            assert all(torch.equal(a, e) for a, e in zip(got, outs)), turn
+
+
+def test_workspaces_that_are_missing_or_too_small_are_refused():
+    x, dy, w, _ = _norm_inputs(1, 50, 64, torch.float32, torch.float32, "shared", 1)
+    stats = torch.ones(1, 50, device="cuda")
+    dx, dw = torch.empty_like(x), torch.empty_like(w)
+    need = clear._workspace_bytes("clear_layer_norm_bwd_workspace", 0, 1, 50, 64, 0)
+    ws = torch.empty(need + 16, dtype=torch.uint8, device="cuda")
+    stream = torch.cuda.current_stream().cuda_stream
+
+    def norm(ptr, n):
+        return clear.load().clear_layer_norm_bwd(x.data_ptr(), dy.data_ptr(), w.data_ptr(), stats.data_ptr(), stats.data_ptr(),
+                                                 dx.data_ptr(), dw.data_ptr(), None, 1, 50, 64, clear.F32, clear.F32, 0, 0, 64, 0, 64,
+                                                 0, 64, 0, 0, 0, 0.0, ptr, n, stream)
+
+    assert norm(None, need) == norm(ws.data_ptr(), need - 1) == clear.ERR_INVALID_ARG
+    assert norm(ws.data_ptr() + 4, need) == clear.ERR_MISALIGNED
+    assert norm(ws.data_ptr(), need) == clear.OK
+    q = _randn((1, 1, 5, 64), 1)
+    outs = [torch.empty_like(q) for _ in range(2)]
+    dg = torch.empty(64, device="cuda")
+    need = clear._workspace_bytes("clear_qk_norm_rope_bwd_workspace", 0, 64)
+    ws = torch.empty(need + 16, dtype=torch.uint8, device="cuda")
+
+    def prep(ptr, n):
+        return clear.load().clear_qk_norm_rope_bwd(q.data_ptr(), q.data_ptr(), q.data_ptr(), q.data_ptr(), outs[0].data_ptr(),
+                                                   outs[1].data_ptr(), None, None, dg.data_ptr(), None, 1, 1, 2, 2, 1, 64, clear.F32,
+                                                   8, 28, 28, 10000.0, 1.0, 1e-6, 1.0, ptr, n, stream)
+
+    assert prep(None, need) == prep(ws.data_ptr(), need - 1) == clear.ERR_INVALID_ARG
+    assert prep(ws.data_ptr() + 8, need) == clear.ERR_MISALIGNED and prep(ws.data_ptr(), need) == clear.OK
+    torch.cuda.synchronize()
+
+
+# ---- the operators together ------------------------------------------------------------------------------------------
+
+
+def test_a_layer_forward_and_backward():
+    """Residual rows -> modulated layer norm -> projection -> Q/K preparation -> attention, and back to the rows, the modulation and the
+    gains, in fp32 against autograd of the same layer in 64 bits.  Every stage is good to 1e-4 of its result (the attention's
+    gradients to 1e-4 of the largest is the loosest), so the chain's few stages are to 1e-3 of the norm."""
+    B, H, gh, gw, T, d, r = 2, 2, 6, 7, 5, 64, 3.0
+    N, C, axes = T + gh * gw, 2 * 64, (8, 28, 28)
+    x, proj = _randn((B, N, C), 1), _randn((C, 3 * C), 2) / math.sqrt(C)
+    scale, shift, dout = 0.3 * _randn((B, C), 3), 0.3 * _randn((B, C), 4), _randn((B, H, N, d), 5)
+    gq, gk = 1.0 + 0.2 * _randn((d,), 6), 1.0 + 0.2 * _randn((d,), 7)
+
+    y, mean, rstd = torch.empty_like(x), torch.empty(B, N, device="cuda"), torch.empty(B, N, device="cuda")
+    clear.clear_layer_norm_fwd(x, y, scale, shift, mean, rstd, weight_offset=1.0)
+    heads = (y.double() @ proj.double()).float().view(B, N, 3, H, d).permute(2, 0, 3, 1, 4).contiguous()
+    q, k, v = heads
+    qr, kr, out = torch.empty_like(q), torch.empty_like(q), torch.empty_like(q)
+    clear.clear_qk_norm_rope(q, k, qr, kr, gh, gw, T, axes, gq, gk)
+    clear.clear_attn_fwd_f32(qr, kr, v, out, gh, gw, T, r, d ** -0.5)
+    dqr, dkr, dq, dk, dv = (torch.empty_like(q) for _ in range(5))
+    clear.clear_attn_bwd_f32(qr, kr, v, dout, dqr, dkr, dv, gh, gw, T, r, d ** -0.5)
+    dgq, dgk = torch.empty_like(gq), torch.empty_like(gk)
+    clear.clear_qk_norm_rope_bwd(q, k, dqr, dkr, dq, dk, gh, gw, T, axes, gq, gk, dgq, dgk)
+    dy = (torch.stack((dq, dk, dv)).permute(1, 3, 0, 2, 4).reshape(B, N, 3 * C).double() @ proj.double().t()).float()
+    dx, dscale, dshift = clear.clear_layer_norm_bwd(x, dy, scale, mean, rstd, torch.empty_like(x), torch.empty_like(scale),
+                                                    torch.empty_like(shift), weight_offset=1.0)
+
+    leaves = [t.cpu().double().requires_grad_() for t in (x, scale, shift, gq, gk)]
+    lx, lscale, lshift, lgq, lgk = leaves
+    h = (lx - lx.mean(-1, keepdim=True)) / torch.sqrt(lx.var(-1, correction=0, keepdim=True) + 1e-6)
+    h = h * (1 + lscale[:, None]) + lshift[:, None]
+    tq, tk, tv = (h @ proj.cpu().double()).view(B, N, 3, H, d).permute(2, 0, 3, 1, 4)
+    pos = torch.from_numpy(oracle_prep.token_positions(gh, gw, T)).double()
+    angle = torch.cat([pos[:, a:a + 1] * torch.from_numpy(oracle.frequencies(n, 10000.0)) for a, n in enumerate(axes)], -1)
+
+    def prepared(t, g):
+        t = t / torch.sqrt(t.square().mean(-1, keepdim=True) + 1e-6) * g
+        return torch.view_as_real(torch.view_as_complex(t.unflatten(-1, (-1, 2)).contiguous()) * torch.exp(1j * angle)).flatten(-2)
+
+    allowed = torch.ones(N, N, dtype=torch.bool)
+    p = pos[T:, 1:]
+    allowed[T:, T:] = ((p[:, None] - p[None]) ** 2).sum(-1) < r * r
+    s = prepared(tq, lgq) @ prepared(tk, lgk).transpose(-1, -2) * d ** -0.5
+    o = torch.softmax(s.masked_fill(~allowed, -math.inf), -1) @ tv
+    grads = torch.autograd.grad(o, leaves, dout.cpu().double())
+
+    def near(got, want):
+        return float((got.cpu().double() - want).norm() / want.norm()) <= 1e-3
+
+    assert near(out, o.detach())
+    for name, got, want in zip(("x", "scale", "shift", "gain_q", "gain_k"), (dx, dscale, dshift, dgq, dgk), grads):
+        assert near(got, want), name
+
+
+def test_rotated_heads_out_of_a_projection_through_the_attention_call():
+    """A packed bf16 projection -> rotary positions head by head -> attention, and the gradient back into a packed tensor."""
+    B, H, gh, gw, T, d, r = 1, 3, 16, 16, 16, 64, 4.0
+    N, axes = T + gh * gw, (8, 28, 28)
+    rows = _randn((B, N, 3, H, d), 1, torch.bfloat16)
+    q, k, v = rows.permute(2, 0, 3, 1, 4)
+    positions = torch.from_numpy(oracle_prep.token_positions(gh, gw, T)).cuda().unsqueeze(0)
+    freqs = torch.cat([clear.clear_rope_frequencies(n) for n in axes])
+    qr, kr, vc = (torch.empty(B, H, N, d, device="cuda", dtype=torch.bfloat16) for _ in range(3))
+    clear.clear_rope_fwd(q, k, qr, kr, positions, freqs, axes)
+    vc.copy_(v)
+    out, dout = torch.empty_like(qr), _randn((B, H, N, d), 2, torch.bfloat16)
+    clear.clear_attn_fwd(qr, kr, vc, out, gh, gw, T, r, d ** -0.5)
+    dqr, dkr, dv = (torch.empty_like(qr) for _ in range(3))
+    clear.clear_attn_bwd_bf16_tc(qr, kr, vc, dout, dqr, dkr, dv, gh, gw, T, r, d ** -0.5)
+    grads = torch.zeros_like(rows)
+    dq, dk, _ = grads.permute(2, 0, 3, 1, 4)
+    clear.clear_rope_bwd(dqr, dkr, dq, dk, positions, freqs, axes)
+    pos = positions.cpu().numpy()
+    for got, src in ((dq, dqr), (dk, dkr)):
+        want = oracle.rotate(_np(src), pos, freqs.numpy(), axes, False, 1.0, inverse=True)
+        _close(got, want, 10 * U * np.abs(_np(src)).max() * 2, torch.bfloat16)
+    from oracle import clear_oracle
+    turned = [torch.from_numpy(oracle.rotate(_np(t), pos, freqs.numpy(), axes, False, 1.0)) for t in (q, k)]
+    want = clear_oracle.attn(*turned, v.contiguous().cpu().double(), gh, gw, T, r, d ** -0.5)
+    # the attention's own bound, and bf16 rotated Q and K: scores off by 2^-7 of a few units at worst, typically far less
+    err = np.abs(_np(out) - np.asarray(want))
+    assert err.max() <= 4e-2 and err.mean() <= 3e-3

@@ -1,0 +1,251 @@
+"""Layer norm, rotary positions and the gradient of the Q/K preparation without a GPU: argument checks through the raw C symbols
+(every call here is refused, or has nothing to do, before any CUDA call; the pointers are never dereferenced), the host arithmetic of
+`clear_rope_frequencies`, the binding's own checks, and pins of the fp64 oracle."""
+import ctypes
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from oracle import clear_oracle_layer as oracle
+from oracle import clear_oracle_qk_prep as oracle_prep
+from paper_2412_16112_b200 import binding as clear
+
+FAKE = 0x10000  # aligned, never touched
+OTHER = [0x20000 + 0x10000 * i for i in range(8)]
+
+
+# ---- refusals --------------------------------------------------------------------------------------------------------
+
+
+def _norm_fwd(x=FAKE, y=OTHER[0], w=None, b=None, mean=None, rstd=None, B=2, N=3, C=8, dtype=clear.BF16, pdtype=clear.F32,
+              xs=(24, 8), ys=(24, 8), ws=0, bs=0, offset=0.0, eps=1e-6):
+    return clear.load().clear_layer_norm_fwd(x, y, w, b, mean, rstd, B, N, C, dtype, pdtype, *xs, *ys, ws, bs, offset, eps, None)
+
+
+@pytest.mark.parametrize("kw", [
+    dict(B=-1), dict(N=-1), dict(C=0), dict(dtype=5), dict(pdtype=5), dict(dtype=clear.F32, pdtype=clear.BF16),
+    dict(eps=-1.0), dict(eps=float("nan")), dict(offset=float("inf")), dict(x=None), dict(y=None),
+    dict(y=FAKE, ys=(48, 16)),                 # in place under other strides
+    dict(ys=(0, 8)), dict(ys=(24, 0)),         # rows of the output on one another
+])
+def test_layer_norm_fwd_refuses(kw):
+    assert _norm_fwd(**kw) == clear.ERR_INVALID_ARG
+
+
+def test_layer_norm_fwd_other_refusals_and_nothing_to_do():
+    assert _norm_fwd(B=65536, N=65536) == clear.ERR_UNSUPPORTED
+    for kw in (dict(x=FAKE + 1), dict(y=FAKE + 1), dict(w=FAKE + 2), dict(b=FAKE + 2), dict(mean=FAKE + 2), dict(rstd=FAKE + 1)):
+        assert _norm_fwd(**kw) == clear.ERR_MISALIGNED
+    assert _norm_fwd(N=0, x=None, y=None) == clear.OK and _norm_fwd(B=0, x=None, y=None) == clear.OK
+
+
+def _norm_bwd(x=FAKE, dy=OTHER[0], w=None, mean=OTHER[1], rstd=OTHER[2], dx=OTHER[3], dw=None, db=None, B=2, N=3, C=8,
+              dtype=clear.BF16, pdtype=clear.F32, per_batch=0, xs=(24, 8), dys=(24, 8), dxs=(24, 8), ws=0, dws=0, dbs=0, offset=0.0,
+              work=None, n_work=0):
+    return clear.load().clear_layer_norm_bwd(x, dy, w, mean, rstd, dx, dw, db, B, N, C, dtype, pdtype, per_batch, *xs, *dys, *dxs, ws,
+                                             dws, dbs, offset, work, n_work, None)
+
+
+@pytest.mark.parametrize("kw", [
+    dict(B=-1), dict(N=-2), dict(C=0), dict(dtype=-1), dict(dtype=clear.F32, pdtype=clear.BF16), dict(offset=float("nan")),
+    dict(x=None), dict(dy=None), dict(dx=None), dict(mean=None), dict(rstd=None),
+    dict(dx=FAKE, dxs=(48, 16)), dict(dx=OTHER[0], dxs=(48, 16)), dict(dxs=(24, 0)),
+    dict(w=OTHER[4], ws=8), dict(dw=OTHER[4], dws=8), dict(db=OTHER[4], dbs=8),          # shared weights have no stride
+    dict(per_batch=1, dw=OTHER[4], dws=0), dict(per_batch=1, db=OTHER[4], dbs=0),        # sums of entries on one another
+    dict(dw=OTHER[4], db=OTHER[4]),
+])
+def test_layer_norm_bwd_refuses(kw):
+    assert _norm_bwd(**kw) == clear.ERR_INVALID_ARG
+
+
+def test_layer_norm_bwd_other_refusals():
+    assert _norm_bwd(B=70000, N=2, per_batch=1) == clear.ERR_UNSUPPORTED
+    assert _norm_bwd(B=65536, N=65536) == clear.ERR_UNSUPPORTED
+    for kw in (dict(x=FAKE + 1), dict(dy=FAKE + 1), dict(dx=FAKE + 1), dict(w=FAKE + 2), dict(dw=FAKE + 2), dict(db=FAKE + 2),
+               dict(mean=FAKE + 2), dict(rstd=FAKE + 2)):
+        assert _norm_bwd(**kw) == clear.ERR_MISALIGNED
+    assert _norm_bwd(N=0, x=None, dy=None, dx=None) == clear.OK
+    n = ctypes.c_size_t()
+    f = clear.load().clear_layer_norm_bwd_workspace
+    assert f(1, 1, 0, 0, ctypes.byref(n)) == f(-1, 1, 8, 0, ctypes.byref(n)) == f(1, 1, 8, 0, None) == clear.ERR_INVALID_ARG
+    assert f(70000, 1, 8, 1, ctypes.byref(n)) == clear.ERR_UNSUPPORTED
+    assert f(0, 5, 8, 0, ctypes.byref(n)) == clear.OK and n.value == 0
+
+
+def _rope(q=FAKE, k=OTHER[0], qo=OTHER[1], ko=OTHER[2], strides=None, pos=OTHER[3], pb=0, pn=1, bits=32, freqs=(1.0, 0.1, 0.01, 0.001),
+          axes=(8,), B=2, H=3, Hk=1, N=5, d=8, dtype=clear.BF16, layout=clear.ROPE_HALF, factor=1.0, fn="clear_rope_fwd"):
+    if strides is None:
+        strides = 2 * [3 * 40, 40, 8] + 2 * [40, 40, 8]
+    s = (ctypes.c_longlong * 12)(*strides) if strides else None
+    f = (ctypes.c_double * max(1, len(freqs)))(*freqs) if freqs is not None else None
+    a = (ctypes.c_int * len(axes))(*axes) if axes else None
+    return getattr(clear.load(), fn)(q, k, qo, ko, s, pos, pb, pn, bits, f, a, len(axes), B, H, Hk, N, d, dtype, layout, factor, None)
+
+
+@pytest.mark.parametrize("fn", ["clear_rope_fwd", "clear_rope_bwd"])
+@pytest.mark.parametrize("kw", [
+    dict(B=-1), dict(N=-1), dict(H=0), dict(Hk=0), dict(d=0), dict(dtype=9), dict(layout=2), dict(bits=16), dict(strides=[]),
+    dict(freqs=None), dict(axes=()), dict(axes=(7,)), dict(axes=(-2, 8)), dict(axes=(8, 2)), dict(axes=(0, 0)),
+    dict(freqs=(1.0, float("nan"), 1.0, 1.0)), dict(freqs=(float("inf"), 1.0, 1.0, 1.0)), dict(factor=float("nan")),
+    dict(q=None), dict(qo=None), dict(ko=None), dict(k=None), dict(pos=None),
+    dict(qo=FAKE, strides=[120, 40, 8, 40, 80, 8, 40, 40, 8, 40, 40, 8]),      # in place under other strides
+    dict(strides=[120, 40, 8, 0, 40, 8, 40, 40, 8, 40, 40, 8]),                # rows of the output on one another
+    dict(strides=[120, 40, 8, 120, 0, 8, 40, 40, 8, 40, 40, 8]),
+    dict(strides=[120, 40, 8, 120, 40, 8, 40, 40, 8, 40, 40, 0]),
+    dict(ko=OTHER[1]), dict(qo=OTHER[0]), dict(ko=FAKE),
+])
+def test_rope_refuses(fn, kw):
+    assert _rope(fn=fn, **kw) == clear.ERR_INVALID_ARG
+
+
+def test_rope_other_refusals_and_nothing_to_do():
+    assert _rope(d=258) == clear.ERR_UNSUPPORTED
+    assert _rope(axes=(2, 2, 2, 2, 0, 0, 0, 0, 0)) == clear.ERR_UNSUPPORTED
+    for kw in (dict(q=FAKE + 1), dict(ko=OTHER[2] + 1), dict(pos=OTHER[3] + 2), dict(pos=OTHER[3] + 4, bits=64),
+               dict(dtype=clear.F32, qo=OTHER[1] + 2)):
+        assert _rope(**kw) == clear.ERR_MISALIGNED
+    assert _rope(N=0, q=None, qo=None, pos=None) == clear.OK and _rope(B=0) == clear.OK
+
+
+def _prep_bwd(q=FAKE, k=OTHER[0], dqr=OTHER[1], dkr=OTHER[2], dq=OTHER[3], dk=OTHER[4], gq=None, gk=None, dgq=None, dgk=None, B=1, H=2,
+              gh=4, gw=4, T=1, d=128, dtype=clear.BF16, axes=(16, 56, 56), theta=10000.0, ntk=1.0, eps=1e-6, qf=1.0, work=None,
+              n_work=0):
+    return clear.load().clear_qk_norm_rope_bwd(q, k, dqr, dkr, dq, dk, gq, gk, dgq, dgk, B, H, gh, gw, T, d, dtype, *axes, theta, ntk,
+                                               eps, qf, work, n_work, None)
+
+
+@pytest.mark.parametrize("kw", [
+    dict(B=0), dict(H=-1), dict(gh=0), dict(gw=0), dict(T=-1), dict(dtype=7), dict(axes=(15, 57, 56)), dict(axes=(16, 56, 54)),
+    dict(axes=(-2, 66, 64)), dict(theta=0.0), dict(theta=float("inf")), dict(ntk=0.0), dict(ntk=float("nan")), dict(eps=-1e-6),
+    dict(eps=float("nan")), dict(qf=float("inf")), dict(q=None), dict(k=None), dict(dqr=None), dict(dkr=None), dict(dq=None),
+    dict(dk=None), dict(dk=OTHER[3]), dict(dq=OTHER[0]), dict(dq=OTHER[2]), dict(dk=FAKE), dict(dk=OTHER[1]),
+    dict(dgq=OTHER[5], dgk=OTHER[5]),
+])
+def test_prep_gradient_refuses(kw):
+    assert _prep_bwd(**kw) == clear.ERR_INVALID_ARG
+
+
+def test_prep_gradient_other_refusals():
+    assert _prep_bwd(d=96, axes=(16, 40, 40)) == clear.ERR_UNSUPPORTED
+    for kw in (dict(k=OTHER[0] + 8), dict(dq=OTHER[3] + 4), dict(gq=FAKE + 2), dict(dgk=FAKE + 2)):
+        assert _prep_bwd(**kw) == clear.ERR_MISALIGNED
+    n = ctypes.c_size_t()
+    f = clear.load().clear_qk_norm_rope_bwd_workspace
+    assert f(64, None) == f(0, ctypes.byref(n)) == clear.ERR_INVALID_ARG and f(96, ctypes.byref(n)) == clear.ERR_UNSUPPORTED
+
+
+def test_the_binding_refuses_before_the_library_is_asked():
+    x = torch.zeros(2, 3, 8)
+    with pytest.raises(ValueError):
+        clear.clear_layer_norm_fwd(x, torch.empty_like(x))                       # not on a GPU
+    with pytest.raises(ValueError):
+        clear.clear_rope_fwd(torch.zeros(1, 1, 2, 8), None, torch.zeros(1, 1, 2, 8), None, torch.zeros(1, 2, 1, dtype=torch.int32),
+                             clear.clear_rope_frequencies(8), (8,))
+    with pytest.raises(ValueError):
+        clear.clear_qk_norm_rope_bwd(*[torch.zeros(1, 1, 5, 64)] * 6, 2, 2, 1, (8, 28, 28))
+
+
+# ---- frequencies -----------------------------------------------------------------------------------------------------
+
+
+@pytest.mark.parametrize("dim", [2, 4, 40, 128])
+@pytest.mark.parametrize("scaling", ["none", "linear", "ntk", "parts"])
+def test_frequencies_match_the_oracle(dim, scaling):
+    code = getattr(clear, "ROPE_SCALE_" + scaling.upper())
+    got = clear.clear_rope_frequencies(dim, 500.0, code, 8.0, 4096.0, 32.0, 1.0).numpy()
+    want = oracle.frequencies(dim, 500.0, scaling, 8.0, 4096.0, 32.0, 1.0)
+    np.testing.assert_allclose(got, want, rtol=1e-13)   # a few roundings of 64 bits each, pow's among them
+
+
+def test_frequencies_ends():
+    f = clear.clear_rope_frequencies
+    plain, ntk = f(64).numpy(), f(64, scaling=clear.ROPE_SCALE_NTK, factor=4.0).numpy()
+    assert plain[0] == 1.0 and ntk[0] == 1.0 and ntk[-1] == pytest.approx(plain[-1] / 4.0, rel=1e-12)
+    parts = f(64, scaling=clear.ROPE_SCALE_PARTS, factor=4.0, trained_length=4096.0).numpy()
+    assert parts[0] == plain[0] and parts[-1] == pytest.approx(plain[-1] / 4.0, rel=1e-12)
+    assert (parts <= plain).all() and (parts >= plain / 4.0 * (1 - 1e-12)).all()
+
+
+@pytest.mark.parametrize("kw", [dict(dim=3), dict(dim=0), dict(dim=-2), dict(theta=0.0), dict(factor=0.0), dict(factor=float("inf")),
+                                dict(scaling=4), dict(scaling=3, trained_length=0.0), dict(scaling=3, fast=1.0, slow=1.0),
+                                dict(scaling=3, slow=-1.0), dict(scaling=3, fast=float("nan"))])
+def test_frequencies_refuse(kw):
+    with pytest.raises(clear.ClearError) as e:
+        clear.clear_rope_frequencies(**{"dim": 8, **kw})
+    assert e.value.status == clear.ERR_INVALID_ARG
+
+
+# ---- pins of the oracle ----------------------------------------------------------------------------------------------
+
+
+def _differences(f, x, dy, h=1e-5):
+    """Central differences of sum(f(x) dy) in every element of x."""
+    g = np.zeros_like(x)
+    for i in np.ndindex(x.shape):
+        up, down = x.copy(), x.copy()
+        up[i] += h
+        down[i] -= h
+        g[i] = ((f(up) - f(down)) * dy).sum() / (2 * h)
+    return g
+
+
+@pytest.mark.parametrize("per_batch", [False, True])
+def test_oracle_layer_norm_and_its_gradient(per_batch):
+    rng = np.random.default_rng(3)
+    B, N, C = 2, 3, 7
+    x, dy = rng.normal(size=(B, N, C)) * 2 + 1, rng.normal(size=(B, N, C))
+    w, b = (rng.normal(size=(B, C) if per_batch else C) for _ in range(2))
+    y, mean, rstd = oracle.layer_norm(x, w, b, 1.0, 1e-3)
+    plain = oracle.layer_norm(x, None, None, 5.0, 0.0)[0]
+    np.testing.assert_allclose(plain.mean(-1), 0, atol=1e-12)
+    np.testing.assert_allclose((plain ** 2).mean(-1), 1, rtol=1e-12)
+    want = torch.nn.functional.layer_norm(torch.from_numpy(x), (C,), eps=1e-3).numpy()
+    wide = (lambda p: p[:, None]) if per_batch else (lambda p: p)
+    np.testing.assert_allclose(y, want * (1 + wide(w)) + wide(b), rtol=1e-11, atol=1e-12)
+    dx, dw, db = oracle.layer_norm_grad(x, dy, w, mean, rstd, 1.0, per_batch)
+    # differences: truncation h^2 times third derivatives of order 10, rounding 1e-16 / h
+    np.testing.assert_allclose(dx, _differences(lambda t: oracle.layer_norm(t, w, b, 1.0, 1e-3)[0], x, dy), atol=1e-7)
+    np.testing.assert_allclose(dw, _differences(lambda t: oracle.layer_norm(x, t, b, 1.0, 1e-3)[0], w, dy), atol=1e-7)
+    np.testing.assert_allclose(db, _differences(lambda t: oracle.layer_norm(x, w, t, 1.0, 1e-3)[0], b, dy), atol=1e-7)
+
+
+@pytest.mark.parametrize("half", [False, True])
+def test_oracle_rotation_and_its_gradient(half):
+    rng = np.random.default_rng(4)
+    B, H, N, d, axes = 2, 2, 3, 10, (2, 6)
+    x, dy = rng.normal(size=(B, H, N, d)), rng.normal(size=(B, H, N, d))
+    pos = rng.integers(-50, 50, size=(B, N, 2))
+    freqs = rng.uniform(0.01, 1.0, size=4)
+    y = oracle.rotate(x, pos, freqs, axes, half, 1.5)
+    # as complex numbers
+    lo, hi = (slice(0, 4), slice(4, 8)) if half else (slice(0, 8, 2), slice(1, 8, 2))
+    angle = np.concatenate([pos[..., :1] * freqs[:1], pos[..., 1:] * freqs[1:]], -1)[:, None]
+    z = (x[..., lo] + 1j * x[..., hi]) * 1.5 * np.exp(1j * angle)
+    np.testing.assert_allclose(y[..., lo], z.real, atol=1e-12)
+    np.testing.assert_allclose(y[..., hi], z.imag, atol=1e-12)
+    assert (y[..., 8:] == x[..., 8:]).all()
+    g = oracle.rotate(dy, pos, freqs, axes, half, 1.5, inverse=True)
+    np.testing.assert_allclose(g, _differences(lambda t: oracle.rotate(t, pos, freqs, axes, half, 1.5), x, dy), atol=1e-7)
+    np.testing.assert_allclose(oracle.rotate(y, pos, freqs, axes, half, 1 / 1.5, inverse=True)[..., :8], x[..., :8], atol=1e-12)
+
+
+def test_oracle_gradient_of_the_preparation():
+    rng = np.random.default_rng(5)
+    gh, gw, T, axes = 2, 2, 1, (2, 2, 4)
+    x, dy = rng.normal(size=(1, 2, 5, 8)), rng.normal(size=(1, 2, 5, 8))
+    gain = rng.uniform(0.5, 1.5, size=8)
+    pos = oracle_prep.token_positions(gh, gw, T)
+
+    def forward(t, g=gain):
+        return oracle_prep.rope(oracle_prep.rms_norm(t, g, 1e-3), pos, axes, 100.0, 3.0) * 0.7
+
+    dx, dgain = oracle.qk_prep_grad(x, dy, gain, pos, axes, 100.0, 3.0, 1e-3, 0.7)
+    np.testing.assert_allclose(dx, _differences(forward, x, dy), atol=1e-7)
+    np.testing.assert_allclose(dgain, _differences(lambda g: forward(x, g), gain, dy), atol=1e-7)
+
+
+def test_oracle_by_parts_is_continuous_and_ordered():
+    a = oracle.frequencies(128, 10000.0, "parts", 8.0, 4096.0)
+    assert (np.diff(a) < 0).all() and a[0] == 1.0 and math.isclose(a[-1] * 8, oracle.frequencies(128, 10000.0)[-1])

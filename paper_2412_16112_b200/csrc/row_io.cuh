@@ -9,6 +9,48 @@
 
 namespace clear {
 
+// Two fp32 values in one 64-bit register pair: the packed instructions do both in one issue slot, which is what rows of bf16 at
+// HBM speed are short of.
+struct F2 {
+    unsigned long long v;
+    __device__ __forceinline__ F2() {}
+    __device__ __forceinline__ F2(float lo, float hi) { asm("mov.b64 %0, {%1, %2};" : "=l"(v) : "f"(lo), "f"(hi)); }
+    explicit __device__ __forceinline__ F2(float both) : F2(both, both) {}
+    __device__ __forceinline__ float lo() const { return __uint_as_float((uint32_t)v); }
+    __device__ __forceinline__ float hi() const { return __uint_as_float((uint32_t)(v >> 32)); }
+};
+__device__ __forceinline__ F2 operator+(F2 a, F2 b)
+{
+    F2 r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v));
+    return r;
+}
+__device__ __forceinline__ F2 operator*(F2 a, F2 b)
+{
+    F2 r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v));
+    return r;
+}
+__device__ __forceinline__ F2 fma2(F2 a, F2 b, F2 c)
+{
+    F2 r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r.v) : "l"(a.v), "l"(b.v), "l"(c.v));
+    return r;
+}
+
+// The same as two registers that need not be neighbours, for values that come one by one.
+struct S2 {
+    float x, y;
+    __device__ __forceinline__ S2() {}
+    __device__ __forceinline__ S2(float lo, float hi) : x(lo), y(hi) {}
+    explicit __device__ __forceinline__ S2(float both) : x(both), y(both) {}
+    __device__ __forceinline__ float lo() const { return x; }
+    __device__ __forceinline__ float hi() const { return y; }
+};
+__device__ __forceinline__ S2 operator+(S2 a, S2 b) { return S2(a.x + b.x, a.y + b.y); }
+__device__ __forceinline__ S2 operator*(S2 a, S2 b) { return S2(a.x * b.x, a.y * b.y); }
+__device__ __forceinline__ S2 fma2(S2 a, S2 b, S2 c) { return S2(fmaf(a.x, b.x, c.x), fmaf(a.y, b.y, c.y)); }
+
 template <int BYTES> struct RawOf;
 template <> struct RawOf<2> { using type = unsigned short; };
 template <> struct RawOf<4> { using type = uint32_t; };

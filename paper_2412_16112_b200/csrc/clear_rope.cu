@@ -1,8 +1,8 @@
 // Rotary positions of Q and K: each pair of channels turns by position * frequency, over all or the first part of a head; the
 // gradient is the turn by the opposite angle.  Pairs are neighbours (2p, 2p+1) or half the rotary part apart (p, p + P).
 //
-// HBM bounds it (every element in once, out once).  A thread owns a few pairs of one token and walks over the heads: angles
-// depend on the token only, so their sines and cosines are computed once and serve all heads of Q and of K.
+// HBM bounds it (every element in once, out once).  A thread owns a few pairs of one token and walks over heads: angles depend on
+// the token only, so their sines and cosines are computed once and serve several heads of Q and of K.
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 
@@ -29,13 +29,15 @@ struct RopeParams {
     RopeTensor t[2];
     const void *positions;
     long long pos_b, pos_n;
-    long long n_items;          // tokens of all batch entries times threads a token
+    long long n_tokens_all;     // tokens of all batch entries
     unsigned n_tokens;          // tokens of a batch entry
-    int pos64;
-    int pairs, turn_items, items;  // pairs of a head; threads a token: turning, all
+    unsigned turn_blocks;       // blocks that turn; those behind them copy
+    int narrow;                 // whether tokens times threads fit 32 bits
+    int copy_v;                 // channels an access of those
+    int pairs, turn_items, copy_items;  // pairs of a head; threads a token
     int heads_a_part;           // heads (of Q and K together) that a thread walks over
     int head_dim;
-    float factor, sign;
+    float factor, sin_factor;
     uint64_t turns[kMaxRopePairs];
     uint8_t axis[kMaxRopePairs];
 };
@@ -85,35 +87,75 @@ struct Turn {
     }
 };
 
-template <typename T, int V, bool HALF>
-__global__ void __launch_bounds__(kRopeThreads) clear_rope_kernel(const __grid_constant__ RopeParams p)
+// V channels of each of a token's heads, four heads at a time.
+template <typename T, int V>
+__device__ __forceinline__ void copy_heads(const T *in, T *out, long long in_h, long long out_h, int heads)
 {
-    constexpr int kRows = 4;  // heads in flight
+    for (int h = 0; h < heads; h += 4) {
+        Pack<T, V> x[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            if (h + j < heads) x[j].load(in + j * in_h);
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            if (h + j < heads) x[j].store(out + j * out_h);
+        in += 4 * in_h;
+        out += 4 * out_h;
+    }
+}
+
+template <typename T, int V, bool HALF, typename Int>
+__global__ void __launch_bounds__(kRopeThreads, 4) clear_rope_kernel(const __grid_constant__ RopeParams p)
+{
+    constexpr int kRows = HALF ? 2 : 4;  // heads in flight: four accesses of a thread
     using Turner = Turn<T, V, HALF>;
-    const long long item = (long long)blockIdx.x * kRopeThreads + threadIdx.x;
-    if (item >= p.n_items) return;
-    const long long token = item / p.items;
-    const int part = (int)(item - token * p.items);
-    const unsigned b = (unsigned)(token / p.n_tokens), n = (unsigned)(token - (long long)b * p.n_tokens);
+    // constants that lanes read at places of their own would come one lane at a time
+    __shared__ uint64_t s_turns[kMaxRopePairs];
+    __shared__ uint8_t s_axis[kMaxRopePairs];
+    for (int i = threadIdx.x; i < p.pairs; i += kRopeThreads) {
+        s_turns[i] = p.turns[i];
+        s_axis[i] = p.axis[i];
+    }
+    __syncthreads();
+    // the first blocks turn, the others copy what does not turn: both kinds of work in one warp would wait for one another
+    const bool turning = blockIdx.x < p.turn_blocks;
+    const int items = turning ? p.turn_items : p.copy_items;  // threads a token
+    const long long item = (long long)(turning ? blockIdx.x : blockIdx.x - p.turn_blocks) * kRopeThreads + threadIdx.x;
+    if (item >= p.n_tokens_all * items) return;
+    unsigned b, n;
+    int part;
+    if (p.narrow) {  // 64-bit divisions take their time
+        const unsigned token = (unsigned)item / (unsigned)items;
+        part = (int)((unsigned)item - token * items);
+        b = token / p.n_tokens;
+        n = token - b * p.n_tokens;
+    } else {
+        const long long token = item / items;
+        part = (int)(item - token * items);
+        b = (unsigned)(token / p.n_tokens);
+        n = (unsigned)(token - (long long)b * p.n_tokens);
+    }
     int h0 = blockIdx.y * p.heads_a_part, h1 = h0 + p.heads_a_part;  // of the heads of Q, then those of K
-    const bool turning = part < p.turn_items;
     Turner turner;
     int first;
     if (turning) {
         const int pair0 = part * Turner::kPairs;
         first = HALF ? pair0 : 2 * pair0;
         const long long at = (long long)b * p.pos_b + (long long)n * p.pos_n;
+        int axis = -1;
+        Int pos = 0;
 #pragma unroll
         for (int i = 0; i < Turner::kPairs; ++i) {
-            const int axis = p.axis[pair0 + i];
-            const int64_t pos = p.pos64 ? static_cast<const int64_t *>(p.positions)[at + axis]
-                                        : (int64_t)static_cast<const int32_t *>(p.positions)[at + axis];
-            turn_sincos(pos, p.turns[pair0 + i], turner.s[i], turner.c[i]);
-            turner.s[i] *= p.factor * p.sign;
+            if (s_axis[pair0 + i] != axis) {
+                axis = s_axis[pair0 + i];
+                pos = static_cast<const Int *>(p.positions)[at + axis];
+            }
+            turn_sincos(pos, s_turns[pair0 + i], turner.s[i], turner.c[i]);
+            turner.s[i] *= p.sin_factor;
             turner.c[i] *= p.factor;
         }
     } else {
-        first = 2 * p.pairs + (part - p.turn_items) * V;
+        first = 2 * p.pairs + part * p.copy_v;
     }
 #pragma unroll
     for (int which = 0; which < 2; ++which) {
@@ -124,67 +166,39 @@ __global__ void __launch_bounds__(kRopeThreads) clear_rope_kernel(const __grid_c
         if (from >= to || !(turning || t.copy)) continue;
         const T *in = static_cast<const T *>(t.in) + (long long)b * t.in_b + (long long)n * t.in_n + from * t.in_h;
         T *out = static_cast<T *>(t.out) + (long long)b * t.out_b + (long long)n * t.out_n + from * t.out_h;
+        if (!turning) {
+            in += first;
+            out += first;
+            if (p.copy_v * sizeof(T) == 16) copy_heads<T, 16 / sizeof(T)>(in, out, t.in_h, t.out_h, to - from);
+            else if (p.copy_v == 4) copy_heads<T, 4>(in, out, t.in_h, t.out_h, to - from);
+            else if (p.copy_v == 2) copy_heads<T, 2>(in, out, t.in_h, t.out_h, to - from);
+            else copy_heads<T, 1>(in, out, t.in_h, t.out_h, to - from);
+            continue;
+        }
         int h = from;
-        if (turning) {
-            for (; h + kRows <= to; h += kRows) {
-                Pack<T, V> x[kRows][Turner::kAccesses];
+        for (; h + kRows <= to; h += kRows) {
+            Pack<T, V> x[kRows][Turner::kAccesses];
 #pragma unroll
-                for (int j = 0; j < kRows; ++j) turner.load(in + j * t.in_h, first, p.pairs, x[j]);
+            for (int j = 0; j < kRows; ++j) turner.load(in + j * t.in_h, first, p.pairs, x[j]);
 #pragma unroll
-                for (int j = 0; j < kRows; ++j) turner.turn_store(out + j * t.out_h, first, p.pairs, x[j]);
-                in += kRows * t.in_h;
-                out += kRows * t.out_h;
-            }
-            for (; h < to; ++h) {
-                Pack<T, V> x[Turner::kAccesses];
-                turner.load(in, first, p.pairs, x);
-                turner.turn_store(out, first, p.pairs, x);
-                in += t.in_h;
-                out += t.out_h;
-            }
-        } else {
-            for (; h + kRows <= to; h += kRows) {
-                Pack<T, V> x[kRows];
-#pragma unroll
-                for (int j = 0; j < kRows; ++j) x[j].load(in + j * t.in_h + first);
-#pragma unroll
-                for (int j = 0; j < kRows; ++j) x[j].store(out + j * t.out_h + first);
-                in += kRows * t.in_h;
-                out += kRows * t.out_h;
-            }
-            for (; h < to; ++h) {
-                Pack<T, V> x;
-                x.load(in + first);
-                x.store(out + first);
-                in += t.in_h;
-                out += t.out_h;
-            }
+            for (int j = 0; j < kRows; ++j) turner.turn_store(out + j * t.out_h, first, p.pairs, x[j]);
+            in += kRows * t.in_h;
+            out += kRows * t.out_h;
+        }
+        for (; h < to; ++h) {
+            Pack<T, V> x[Turner::kAccesses];
+            turner.load(in, first, p.pairs, x);
+            turner.turn_store(out, first, p.pairs, x);
+            in += t.in_h;
+            out += t.out_h;
         }
     }
 }
 
-template <typename T, int V, bool HALF>
-int launch(RopeParams &p, const RopeArgs &a, int n_sm, cudaStream_t stream)
+// Accesses of V channels: rows and heads on their boundary, and the part of the head that begins at `offset`.
+bool fits(const RopeParams &p, int V, size_t elem, int offset)
 {
-    p.turn_items = p.pairs / Turn<T, V, HALF>::kPairs;
-    p.items = p.turn_items + (p.t[0].copy || p.t[1].copy ? (p.head_dim - 2 * p.pairs) / V : 0);
-    p.n_items = (long long)a.B * a.N * p.items;
-    const long long blocks = (p.n_items + kRopeThreads - 1) / kRopeThreads;
-    if (blocks > 0x7fffffffLL) return CLEAR_ERR_UNSUPPORTED;
-    // heads are shared out over blocks only while tokens alone leave SMs without work: every share computes the angles anew
-    const int heads = p.t[0].heads + p.t[1].heads;
-    const int parts = (int)std::min<long long>(heads, std::max<long long>(1, 4LL * n_sm / blocks));
-    p.heads_a_part = (heads + parts - 1) / parts;
-    const unsigned shares = (unsigned)((heads + p.heads_a_part - 1) / p.heads_a_part);
-    clear_rope_kernel<T, V, HALF><<<dim3((unsigned)blocks, shares), kRopeThreads, 0, stream>>>(p);
-    CLEAR_CUDA_TRY(cudaGetLastError());
-    return CLEAR_OK;
-}
-
-// Accesses of V channels: rows on their boundary, and the rotary part (its halves) and the head whole numbers of them.
-bool fits(const RopeParams &p, int V, size_t elem, bool half)
-{
-    if ((half ? p.pairs : 2 * p.pairs) % V || p.head_dim % V) return false;
+    if (offset % V || p.head_dim % V) return false;
     for (const RopeTensor &t : p.t) {
         if (!t.heads) continue;
         if (!aligned_to(t.in, V * elem) || !aligned_to(t.out, V * elem)) return false;
@@ -194,12 +208,38 @@ bool fits(const RopeParams &p, int V, size_t elem, bool half)
     return true;
 }
 
+template <typename T, int V, bool HALF>
+int launch(RopeParams &p, const RopeArgs &a, int n_sm, cudaStream_t stream)
+{
+    p.turn_items = p.pairs / Turn<T, V, HALF>::kPairs;
+    p.copy_v = 16 / (int)sizeof(T);
+    while (p.copy_v > 1 && !fits(p, p.copy_v, sizeof(T), 2 * p.pairs)) p.copy_v /= 2;
+    p.copy_items = p.t[0].copy || p.t[1].copy ? (p.head_dim - 2 * p.pairs) / p.copy_v : 0;
+    p.n_tokens_all = (long long)a.B * a.N;
+    p.narrow = p.n_tokens_all * std::max(p.turn_items, p.copy_items) <= 0xffffffffLL - kRopeThreads;
+    const long long turn_blocks = (p.n_tokens_all * p.turn_items + kRopeThreads - 1) / kRopeThreads;
+    const long long blocks = turn_blocks + (p.n_tokens_all * p.copy_items + kRopeThreads - 1) / kRopeThreads;
+    if (blocks > 0x7fffffffLL) return CLEAR_ERR_UNSUPPORTED;
+    p.turn_blocks = (unsigned)turn_blocks;
+    // Every share of the heads computes the angles anew, which eight heads carry (4608 tokens of 48 heads 21.5 us, all heads in one
+    // share 21.8, four 23.1; 16680 of 24 fp32 heads 43.6, 58.8, 42.9); fewer to a share while SMs would be without work.
+    const int heads = p.t[0].heads + p.t[1].heads;
+    const int parts = (int)std::min<long long>(heads, std::max<long long>((heads + 7) / 8, 4LL * n_sm / blocks));
+    p.heads_a_part = (heads + parts - 1) / parts;
+    const dim3 grid((unsigned)blocks, (unsigned)((heads + p.heads_a_part - 1) / p.heads_a_part));
+    if (a.pos64) clear_rope_kernel<T, V, HALF, int64_t><<<grid, kRopeThreads, 0, stream>>>(p);
+    else clear_rope_kernel<T, V, HALF, int32_t><<<grid, kRopeThreads, 0, stream>>>(p);
+    CLEAR_CUDA_TRY(cudaGetLastError());
+    return CLEAR_OK;
+}
+
 template <typename T, bool HALF>
 int launch_for(RopeParams &p, const RopeArgs &a, int n_sm, cudaStream_t stream)
 {
-    if (sizeof(T) == 2 && fits(p, 8, sizeof(T), HALF)) return launch<T, sizeof(T) == 2 ? 8 : 4, HALF>(p, a, n_sm, stream);
-    if (fits(p, 4, sizeof(T), HALF)) return launch<T, 4, HALF>(p, a, n_sm, stream);
-    if (fits(p, 2, sizeof(T), HALF)) return launch<T, 2, HALF>(p, a, n_sm, stream);
+    const int part = HALF ? p.pairs : 2 * p.pairs;  // where the second half of the pairs begins, or the rest of the head
+    if (sizeof(T) == 2 && fits(p, 8, sizeof(T), part)) return launch<T, sizeof(T) == 2 ? 8 : 4, HALF>(p, a, n_sm, stream);
+    if (fits(p, 4, sizeof(T), part)) return launch<T, 4, HALF>(p, a, n_sm, stream);
+    if (fits(p, 2, sizeof(T), part)) return launch<T, 2, HALF>(p, a, n_sm, stream);
     return launch<T, 1, HALF>(p, a, n_sm, stream);
 }
 
@@ -234,11 +274,10 @@ int launch_rope(const RopeArgs &a, cudaStream_t stream)
     p.positions = a.positions;
     p.pos_b = a.pos_stride_b;
     p.pos_n = a.pos_stride_n;
-    p.pos64 = a.pos64;
     p.n_tokens = (unsigned)a.N;
     p.head_dim = a.head_dim;
     p.factor = a.factor;
-    p.sign = a.inverse ? -1.f : 1.f;
+    p.sin_factor = a.inverse ? -a.factor : a.factor;
     if (a.dtype == CLEAR_BF16)
         return a.half ? launch_for<__nv_bfloat16, true>(p, a, n_sm, stream) : launch_for<__nv_bfloat16, false>(p, a, n_sm, stream);
     return a.half ? launch_for<float, true>(p, a, n_sm, stream) : launch_for<float, false>(p, a, n_sm, stream);

@@ -1,6 +1,6 @@
 // Sine and cosine of position * frequency at any 64-bit position without loss: the frequency is held in turns, as a 64-bit
 // binary fraction w = frac(frequency / 2 pi) * 2^64, so that the product modulo 2^64 is the angle modulo a turn exactly (the
-// fraction's own rounding, 2^-64 of a turn, is all that the position multiplies).  An fp32 product would be off by position *
+// fraction's own rounding, 2^-62 of a turn, is all that the position multiplies).  An fp32 product would be off by position *
 // frequency * 2^-24 radians: 0.06 at position 10^6.
 #pragma once
 
@@ -9,26 +9,45 @@
 
 namespace clear {
 
+// In two doubles: 1 / 2 pi is kept to 106 bits, so that frequencies of many turns lose nothing either.
 inline uint64_t turns_of(double frequency)
 {
-    const long double turns = (long double)frequency / 6.283185307179586476925286766559L;
-    const long double part = turns - std::floor(turns);
-    return part >= 1.0L ? 0u : (uint64_t)std::ldexp(part, 64);
+    constexpr double kHi = 0.15915494309189535, kLo = -9.839338337591243e-18;
+    // to the nearest whole number, which is exact; half turns in 63 bits and a sign
+    auto fraction = [](double x) { return (uint64_t)(int64_t)((x - std::nearbyint(x)) * 9223372036854775808.0) << 1; };
+    const double hi = frequency * kHi, lo = std::fma(frequency, kHi, -hi) + frequency * kLo;
+    return fraction(hi) + fraction(lo);
 }
 
 #ifdef __CUDACC__
-// The quadrant comes off in whole numbers, so what is rounded to fp32 is at most an eighth of a turn (error below 2^-26 rad).
-__device__ __forceinline__ void turn_sincos(int64_t position, uint64_t turns, float &s, float &c)
+// Sine and cosine of an angle of at most an eighth of a turn, theta in radians: the Taylor sums to theta^9 and theta^10, whose next
+// terms are below 2e-9 there.
+__device__ __forceinline__ void small_sincos(float theta, float &s, float &c)
 {
-    const uint64_t t = (uint64_t)position * turns;
-    const uint32_t quadrant = (uint32_t)((t + (1ull << 61)) >> 62);
-    const int32_t rest = (int32_t)((uint32_t)(t >> 32) - (quadrant << 30));  // [-2^29, 2^29) of 2^32 a turn
+    const float z = theta * theta;
+    float p = fmaf(z, 1.f / 362880, -1.f / 5040);
+    p = fmaf(z, p, 1.f / 120);
+    p = fmaf(z, p, -1.f / 6);
+    s = fmaf(theta * z, p, theta);
+    float q = fmaf(z, -1.f / 3628800, 1.f / 40320);
+    q = fmaf(z, q, -1.f / 720);
+    q = fmaf(z, q, 1.f / 24);
+    q = fmaf(z, q, -0.5f);
+    c = fmaf(z, q, 1.f);
+}
+
+// The quadrant comes off in whole numbers, so what is rounded to fp32 is at most an eighth of a turn (error below 2^-25 rad).
+template <typename Int>
+__device__ __forceinline__ void turn_sincos(Int position, uint64_t turns, float &s, float &c)
+{
+    const uint32_t t = (uint32_t)(((uint64_t)(int64_t)position * turns) >> 32);  // 2^32 a turn
+    const uint32_t quadrant = (t + (1u << 29)) >> 30;
+    const int32_t rest = (int32_t)(t - (quadrant << 30));                       // [-2^29, 2^29)
     float sn, cs;
-    sincospif((float)rest * 4.656612873077393e-10f, &sn, &cs);              // 2^-31: half turns
-    const bool swap = quadrant & 1u;
-    const float a = swap ? cs : sn, b = swap ? sn : cs;
-    s = quadrant & 2u ? -a : a;
-    c = (quadrant + 1u) & 2u ? -b : b;
+    small_sincos((float)rest * 1.4629180792671596e-09f, sn, cs);                // 2 pi / 2^32
+    const float a = quadrant & 1u ? cs : sn, b = quadrant & 1u ? sn : cs;
+    s = __uint_as_float(__float_as_uint(a) ^ ((quadrant & 2u) << 30));
+    c = __uint_as_float(__float_as_uint(b) ^ (((quadrant + 1u) & 2u) << 30));
 }
 #endif
 

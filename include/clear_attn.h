@@ -225,7 +225,8 @@ int clear_qk_norm_rope(const void *q_in, const void *k_in, void *q_out, void *k_
  * workspace: clear_qk_norm_rope_bwd_workspace() bytes of device memory, 16-byte aligned, which the call may write until it has
  * ended on the stream (calls that can overlap need one each); may be NULL when neither gain's gradient is wanted.
  * One launch on `stream`, two with a gain's gradient; no allocation, no host synchronisation.
- * Errors: those of clear_qk_norm_rope; INVALID_ARG also for a workspace that is missing or too small. */
+ * Errors: those of clear_qk_norm_rope; INVALID_ARG also for a workspace that is missing or too small; UNSUPPORTED also for 2^31
+ * tokens or more. */
 int clear_qk_norm_rope_bwd(const void *q, const void *k, const void *dq_rot, const void *dk_rot, void *dq, void *dk,
                            const float *gain_q, const float *gain_k, float *dgain_q, float *dgain_k, int B, int H, int grid_h,
                            int grid_w, int n_text, int head_dim, int dtype, int axis0_dim, int axis1_dim, int axis2_dim, float theta,

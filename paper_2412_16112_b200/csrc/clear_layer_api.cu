@@ -236,7 +236,7 @@ int clear_qk_norm_rope_bwd(const void *q, const void *k, const void *dq_rot, con
     }
     if (dq == dk || dq == k || dq == dk_rot || dk == q || dk == dq_rot) return CLEAR_ERR_INVALID_ARG;
     if (misaligned(gain_q, 4) || misaligned(gain_k, 4) || misaligned(dgain_q, 4) || misaligned(dgain_k, 4)) return CLEAR_ERR_MISALIGNED;
-    if ((long long)B * H > 0x7fffffffLL) return CLEAR_ERR_UNSUPPORTED;
+    if ((long long)B * H > 0x7fffffffLL || n_text + (long long)grid_h * grid_w > 0x7fffffffLL) return CLEAR_ERR_UNSUPPORTED;
     if (dgain_q || dgain_k) {
         if (dgain_q == dgain_k) return CLEAR_ERR_INVALID_ARG;
         size_t need = 0;

@@ -333,14 +333,6 @@ __device__ __forceinline__ float warp_sum4(const float (&v)[4], int lane)
     return x;
 }
 
-// Asynchronous copy of BYTES (4, 8 or 16) into shared memory.
-template <int BYTES>
-__device__ __forceinline__ void copy_async(uint32_t dst, const void *src)
-{
-    if constexpr (BYTES == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
-    else asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" ::"r"(dst), "l"(src), "n"(BYTES) : "memory");
-}
-
 template <typename T, typename TP, int V, int VPT, int LANES, int WARPS>
 __global__ void __launch_bounds__(kBwdThreads<T, V, LANES, WARPS>) clear_norm_bwd_kernel(const __grid_constant__ NormParams p)
 {
@@ -362,7 +354,6 @@ __global__ void __launch_bounds__(kBwdThreads<T, V, LANES, WARPS>) clear_norm_bw
     const T *dy = static_cast<const T *>(p.dy) + (long long)blockIdx.x * p.dy_stride_b + first * V;
     T *dx = static_cast<T *>(p.out) + (long long)blockIdx.x * p.out_stride_b + first * V;
     const float *mean = p.mean_in + (size_t)blockIdx.x * p.rows, *rstd = p.rstd_in + (size_t)blockIdx.x * p.rows;
-    ptx::grid_launch_dependents();
     Share rx[U], rd[U];  // without asynchronous copies: the next rows
     float m[U], r[U];
     // rows at `at` into stage `st`; a row beyond the last, or a channel beyond the row, counts as zero
@@ -398,7 +389,7 @@ __global__ void __launch_bounds__(kBwdThreads<T, V, LANES, WARPS>) clear_norm_bw
             px += p.x_stride_n;
             pd += p.dy_stride_n;
         }
-        if constexpr (kAsync) asm volatile("cp.async.commit_group;" ::: "memory");
+        if constexpr (kAsync) copies_commit();
     };
     auto load_stats = [&](unsigned at) {
         const float *pm = mean + at, *pr = rstd + at;
@@ -452,7 +443,7 @@ __global__ void __launch_bounds__(kBwdThreads<T, V, LANES, WARPS>) clear_norm_bw
         float sums[2 * U], scale[U];
         if constexpr (kAsync) {
             load(row + kAhead * stride, st == 0 ? kStages - 1 : st - 1);
-            asm volatile("cp.async.wait_group %0;" ::"n"(kAhead) : "memory");
+            copies_wait<kAhead>();
 #pragma unroll
             for (int u = 0; u < U; ++u)
 #pragma unroll
@@ -543,7 +534,7 @@ __global__ void __launch_bounds__(kBwdThreads<T, V, LANES, WARPS>) clear_norm_bw
     const int mine = LANES < 32 ? threadIdx.x / 32 : grp;
     float *s_sum = reinterpret_cast<float *>(s_ring);  // [kTerms][2][C]
     if constexpr (kAsync) {
-        asm volatile("cp.async.wait_all;" ::: "memory");
+        copies_wait<0>();
         __syncthreads();  // everybody's copies have landed: the ring is free
     }
     if (LANES == 32 || lane < LANES) {
@@ -606,8 +597,8 @@ __global__ void __launch_bounds__(256) clear_norm_columns_kernel(const __grid_co
     out[p.C + col] = db;
 }
 
-// Sums of partial sums [parts][2][C] for each weight, 8 channels and 32 shares of the parts to a block, in a fixed order.  The blocks
-// are small so that they fit beside those of the kernel before and wait there for its end: no launch lies in between.
+// Sums of partial sums [parts][2][C] for each weight, 8 channels and 32 shares of the parts to a block, in a fixed order: all of a
+// thread's few reads are on their way at once (1 us less than blocks of 32 channels).
 constexpr int kReduceThreads = 256, kReduceChannels = 8;
 template <typename TP>
 __global__ void __launch_bounds__(kReduceThreads)

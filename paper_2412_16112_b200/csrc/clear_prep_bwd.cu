@@ -20,119 +20,164 @@ namespace {
 
 constexpr int kThreads = 256, kWarps = kThreads / 32;
 constexpr int kEpl = 8;  // channels a thread
+constexpr int kBlocksPerSm = 2;
 
 struct PrepBwdParams {
     const void *x[2], *dy[2];
     void *dx[2];
     const float *gain[2];
     float *partial;             // [blocks][2][d], or null
-    int n_bh, bh_a_part, parts; // rows of a token, and the shares that blocks take of them
-    int n_text, grid_w;
-    long long n_tokens;
+    int n_bh, bh_a_part;        // rows of a token, and of the shares that blocks take of them
+    unsigned parts, n_text, grid_w, n_tokens;
     float eps, factor[2];
     uint64_t turns[64];
     uint8_t axis[64];
 };
 
+// Rows come ahead by asynchronous copies of each thread's own channels into its own places of shared memory (bf16: 16 bytes, two
+// steps of three rows, 385 us at 4096 px where three rows ahead in registers take 410), or in registers where 8 channels are two
+// accesses (fp32, 4608 tokens of 24 heads, two rows: 58 us, copies 91).
+template <typename T> constexpr bool kAhead = sizeof(T) == 2;
+template <typename T> constexpr int kRowsOf = kAhead<T> ? 3 : 2;
+constexpr int kSteps = 2;
+template <typename T> constexpr int kRingBytes = kAhead<T> ? kSteps * kRowsOf<T> * 2 * kThreads * 16 : 0;
+
+// Even warps have rows of Q, odd ones rows of K, so that a thread keeps one gain and one gain's gradient.
 template <typename T, int D>
-__global__ void __launch_bounds__(kThreads, 2) clear_prep_bwd_kernel(const __grid_constant__ PrepBwdParams p)
+__global__ void __launch_bounds__(kThreads, kBlocksPerSm) clear_prep_bwd_kernel(const __grid_constant__ PrepBwdParams p)
 {
-    constexpr int kLanes = D / kEpl, kTokens = 32 / kLanes, kRows = 2;
-    __shared__ float s_gain[kWarps][kTokens][2][D];
+    constexpr int kLanes = D / kEpl, kTokens = 32 / kLanes, kPairs = kEpl / 2, kRows = kRowsOf<T>;
+    extern __shared__ __align__(16) unsigned char s_ring[];  // [kSteps][kRows][x, dy][kThreads][16]
+    __shared__ float s_gain[kWarps][kTokens][D];
+    __shared__ uint64_t s_turns[D / 2];
+    __shared__ uint8_t s_axis[D / 2];
+    for (int i = threadIdx.x; i < D / 2; i += kThreads) {
+        s_turns[i] = p.turns[i];
+        s_axis[i] = p.axis[i];
+    }
+    __syncthreads();
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, sub = lane / kLanes, c0 = (lane % kLanes) * kEpl;
-    float gain[2][kEpl], dgain[2][kEpl];
+    const int w = warp & 1;
+    const T *x_in = static_cast<const T *>(p.x[w]), *dy_in = static_cast<const T *>(p.dy[w]);
+    T *dx_out = static_cast<T *>(p.dx[w]);
+    const F2 factor(p.factor[w]);
+    F2 gain[kPairs], dgain[kPairs];
 #pragma unroll
-    for (int w = 0; w < 2; ++w)
-#pragma unroll
-        for (int i = 0; i < kEpl; ++i) {
-            gain[w][i] = p.gain[w] ? __ldg(p.gain[w] + c0 + i) : 1.f;
-            dgain[w][i] = 0.f;
-        }
-    const long long stride = p.n_tokens * D, groups = (p.n_tokens + kTokens - 1) / kTokens;
-    for (long long job = (long long)blockIdx.x * kWarps + warp; job < groups * p.parts; job += (long long)gridDim.x * kWarps) {
-        const long long grp = job / p.parts;
+    for (int i = 0; i < kPairs; ++i) {
+        gain[i] = p.gain[w] ? F2(__ldg(p.gain[w] + c0 + 2 * i), __ldg(p.gain[w] + c0 + 2 * i + 1)) : F2(1.f);
+        dgain[i] = F2(0.f);
+    }
+    const long long stride = (long long)p.n_tokens * D;
+    const unsigned jobs = (p.n_tokens + kTokens - 1) / kTokens * p.parts;
+    for (unsigned job = blockIdx.x * (kWarps / 2) + warp / 2; job < jobs; job += gridDim.x * (kWarps / 2)) {
+        const unsigned grp = job / p.parts, raw = grp * kTokens + sub;
         const int bh0 = (int)(job - grp * p.parts) * p.bh_a_part, bh1 = min(p.n_bh, bh0 + p.bh_a_part);
-        const long long raw = grp * kTokens + sub;
         const bool live = raw < p.n_tokens;
-        const long long n = live ? raw : p.n_tokens - 1;  // the lanes stay together for the shuffles; what they add does not count
-        int pos[3] = {0, 0, 0};
-        if (n >= p.n_text) {
-            const long long at = n - p.n_text;
-            pos[1] = (int)(at / p.grid_w);
-            pos[2] = (int)(at - (long long)pos[1] * p.grid_w);
-        }
-        float sn[kEpl / 2], cs[kEpl / 2];
-#pragma unroll
-        for (int i = 0; i < kEpl / 2; ++i) {
-            const int axis = p.axis[c0 / 2 + i];
-            turn_sincos(axis == 1 ? pos[1] : axis == 2 ? pos[2] : 0, p.turns[c0 / 2 + i], sn[i], cs[i]);
-        }
-        const long long elem = n * D + c0;
-        auto row = [&](auto which, const Pack<T, kEpl> &rx, const Pack<T, kEpl> &rd, long long at) {
-            constexpr int w = decltype(which)::value;
-            float x[kEpl], u[kEpl];
-            rx.get(x);
-            rd.get(u);
-            float ss = 0.f, sx = 0.f;
-#pragma unroll
-            for (int i = 0; i < kEpl / 2; ++i) {
-                const float a = u[2 * i] * p.factor[w], b = u[2 * i + 1] * p.factor[w];
-                u[2 * i] = a * cs[i] + b * sn[i];
-                u[2 * i + 1] = b * cs[i] - a * sn[i];
-            }
-#pragma unroll
-            for (int i = 0; i < kEpl; ++i) {
-                ss = fmaf(x[i], x[i], ss);
-                sx = fmaf(u[i] * gain[w][i], x[i], sx);
-            }
-#pragma unroll
-            for (int off = kLanes / 2; off > 0; off >>= 1) {
-                ss += __shfl_xor_sync(0xffffffffu, ss, off);
-                sx += __shfl_xor_sync(0xffffffffu, sx, off);
-            }
-            const float inv = rsqrtf(fmaf(ss, 1.f / D, p.eps)), along = sx * (1.f / D) * inv * inv;
-            if (live) {
-                Pack<T, kEpl> out;
-#pragma unroll
-                for (int i = 0; i < kEpl; ++i) {
-                    dgain[w][i] = fmaf(u[i], x[i] * inv, dgain[w][i]);
-                    u[i] = inv * (u[i] * gain[w][i] - x[i] * along);
-                }
-                out.set(u);
-                out.store(static_cast<T *>(p.dx[w]) + at);
-            }
+        const unsigned n = live ? raw : p.n_tokens - 1;  // the lanes stay together for the shuffles; what they add does not count
+        const long long elem = (long long)n * D + c0;
+        Pack<T, kEpl> nx[kRows], nd[kRows];
+        auto slot = [&](int step, int j, int which) {
+            return reinterpret_cast<T *>(s_ring + (((step * kRows + j) * 2 + which) * kThreads + threadIdx.x) * 16);
         };
-        for (int bh = bh0; bh < bh1; bh += kRows) {
-            Pack<T, kEpl> rx[2][kRows], rd[2][kRows];
+        auto fetch = [&](int bh, int step) {
 #pragma unroll
-            for (int j = 0; j < kRows; ++j) {
-                const long long at = elem + (long long)min(bh + j, bh1 - 1) * stride;
-#pragma unroll
-                for (int w = 0; w < 2; ++w) {
-                    rx[w][j].load(static_cast<const T *>(p.x[w]) + at);
-                    rd[w][j].load(static_cast<const T *>(p.dy[w]) + at);
-                }
-            }
-#pragma unroll
-            for (int j = 0; j < kRows; ++j) {
+            for (int j = 0; j < kRows; ++j)
                 if (bh + j < bh1) {
                     const long long at = elem + (long long)(bh + j) * stride;
-                    row(std::integral_constant<int, 0>{}, rx[0][j], rd[0][j], at);
-                    row(std::integral_constant<int, 1>{}, rx[1][j], rd[1][j], at);
+                    if constexpr (kAhead<T>) {
+                        copy_async<16>(ptx::smem_u32(slot(step, j, 0)), x_in + at);
+                        copy_async<16>(ptx::smem_u32(slot(step, j, 1)), dy_in + at);
+                    } else {
+                        nx[j].load(x_in + at);
+                        nd[j].load(dy_in + at);
+                    }
+                }
+            if constexpr (kAhead<T>) copies_commit();
+        };
+#pragma unroll
+        for (int s = 0; s < (kAhead<T> ? kSteps - 1 : 1); ++s) fetch(bh0 + s * kRows, s);
+        int pos[3] = {0, 0, 0};
+        if (n >= p.n_text) {
+            pos[1] = (int)((n - p.n_text) / p.grid_w);
+            pos[2] = (int)(n - p.n_text) - pos[1] * (int)p.grid_w;
+        }
+        float sn[kPairs], cs[kPairs];
+#pragma unroll
+        for (int i = 0; i < kPairs; ++i) {
+            const int axis = s_axis[c0 / 2 + i];
+            turn_sincos(axis == 1 ? pos[1] : axis == 2 ? pos[2] : 0, s_turns[c0 / 2 + i], sn[i], cs[i]);
+        }
+        int step = 0;
+        for (int bh = bh0; bh < bh1; bh += kRows) {
+            if constexpr (kAhead<T>) {
+                fetch(bh + (kSteps - 1) * kRows, step == 0 ? kSteps - 1 : step - 1);
+                copies_wait<kSteps - 1>();
+            }
+            F2 x2[kRows][kPairs], u2[kRows][kPairs];
+            float ss[kRows], sx[kRows];
+#pragma unroll
+            for (int j = 0; j < kRows; ++j) {
+                if constexpr (kAhead<T>) {  // beyond the last row: what lies there is not used
+                    nx[j].load(slot(step, j, 0));
+                    nd[j].load(slot(step, j, 1));
+                }
+                float x[kEpl], u[kEpl];
+                nx[j].get(x);
+                nd[j].get(u);
+                F2 squares(0.f), products(0.f);
+#pragma unroll
+                for (int i = 0; i < kPairs; ++i) {
+                    const float a = u[2 * i], b = u[2 * i + 1];
+                    u2[j][i] = F2(fmaf(b, sn[i], a * cs[i]), fmaf(-a, sn[i], b * cs[i])) * factor;
+                    x2[j][i] = F2(x[2 * i], x[2 * i + 1]);
+                    squares = fma2(x2[j][i], x2[j][i], squares);
+                    products = fma2(u2[j][i] * gain[i], x2[j][i], products);
+                }
+                ss[j] = squares.lo() + squares.hi();
+                sx[j] = products.lo() + products.hi();
+            }
+            if (++step == kSteps) step = 0;
+            if constexpr (!kAhead<T>) fetch(bh + kRows, 0);
+#pragma unroll
+            for (int off = kLanes / 2; off > 0; off >>= 1)
+#pragma unroll
+                for (int j = 0; j < kRows; ++j) {
+                    ss[j] += __shfl_xor_sync(0xffffffffu, ss[j], off);
+                    sx[j] += __shfl_xor_sync(0xffffffffu, sx[j], off);
+                }
+#pragma unroll
+            for (int j = 0; j < kRows; ++j) {
+                if (bh + j < bh1 && live) {
+                    const float inv = rsqrtf(fmaf(ss[j], 1.f / D, p.eps));
+                    const F2 inv2(inv), along(-(sx[j] * inv) * (1.f / D) * inv * inv);  // in an order that stays in range
+                    float o[kEpl];
+#pragma unroll
+                    for (int i = 0; i < kPairs; ++i) {
+                        const F2 ui = u2[j][i] * inv2;
+                        dgain[i] = fma2(ui, x2[j][i], dgain[i]);
+                        const F2 r = fma2(x2[j][i], along, ui * gain[i]);
+                        o[2 * i] = r.lo();
+                        o[2 * i + 1] = r.hi();
+                    }
+                    Pack<T, kEpl> out;
+                    out.set(o);
+                    out.store(dx_out + elem + (long long)(bh + j) * stride);
                 }
             }
         }
+        if constexpr (kAhead<T>) copies_wait<0>();
     }
     if (!p.partial) return;
 #pragma unroll
-    for (int w = 0; w < 2; ++w)
-#pragma unroll
-        for (int i = 0; i < kEpl; ++i) s_gain[warp][sub][w][c0 + i] = dgain[w][i];
+    for (int i = 0; i < kPairs; ++i) {
+        s_gain[warp][sub][c0 + 2 * i] = dgain[i].lo();
+        s_gain[warp][sub][c0 + 2 * i + 1] = dgain[i].hi();
+    }
     __syncthreads();
     for (int i = threadIdx.x; i < 2 * D; i += kThreads) {
         float sum = 0.f;
 #pragma unroll
-        for (int k = 0; k < kWarps * kTokens; ++k) sum += s_gain[k / kTokens][k % kTokens][i / D][i % D];
+        for (int k = 0; k < kWarps / 2 * kTokens; ++k) sum += s_gain[2 * (k / kTokens) + i / D][k % kTokens][i % D];
         p.partial[(size_t)blockIdx.x * 2 * D + i] = sum;
     }
 }
@@ -155,7 +200,7 @@ int grid_size(int *blocks)
     int dev = 0, n_sm = 0;
     CLEAR_CUDA_TRY(cudaGetDevice(&dev));
     CLEAR_CUDA_TRY(cudaDeviceGetAttribute(&n_sm, cudaDevAttrMultiProcessorCount, dev));
-    *blocks = 2 * n_sm;
+    *blocks = kBlocksPerSm * n_sm;
     return CLEAR_OK;
 }
 
@@ -163,13 +208,15 @@ template <typename T, int D>
 int launch(PrepBwdParams &p, float *dgain_q, float *dgain_k, int most, cudaStream_t stream)
 {
     constexpr int kTokens = 32 / (D / kEpl);
-    const long long groups = (p.n_tokens + kTokens - 1) / kTokens, warps = (long long)most * kWarps;
+    const int groups = (int)((p.n_tokens + kTokens - 1) / kTokens), warps = most * (kWarps / 2);
     // the rows of a token are shared out while tokens alone leave warps without work
-    p.parts = (int)std::min<long long>(p.n_bh, std::max<long long>(1, warps / groups));
-    p.bh_a_part = (p.n_bh + p.parts - 1) / p.parts;
-    p.parts = (p.n_bh + p.bh_a_part - 1) / p.bh_a_part;
-    const int blocks = (int)std::min<long long>(most, (groups * p.parts + kWarps - 1) / kWarps);
-    clear_prep_bwd_kernel<T, D><<<blocks, kThreads, 0, stream>>>(p);
+    const int parts = std::min(p.n_bh, std::max(1, warps / groups));
+    p.bh_a_part = (p.n_bh + parts - 1) / parts;
+    p.parts = (unsigned)((p.n_bh + p.bh_a_part - 1) / p.bh_a_part);
+    const int blocks = (int)std::min<long long>(most, ((long long)groups * p.parts + kWarps / 2 - 1) / (kWarps / 2));
+    constexpr int smem = kRingBytes<T>;
+    if (smem) CLEAR_CUDA_TRY(cudaFuncSetAttribute(clear_prep_bwd_kernel<T, D>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
+    clear_prep_bwd_kernel<T, D><<<blocks, kThreads, smem, stream>>>(p);
     CLEAR_CUDA_TRY(cudaGetLastError());
     if (!p.partial) return CLEAR_OK;
     cudaLaunchConfig_t cfg{};
@@ -209,9 +256,9 @@ int launch_prep_bwd(const void *q, const void *k, const void *dq_rot, const void
     p.gain[0] = gain_q; p.gain[1] = gain_k;
     p.partial = dgain_q || dgain_k ? static_cast<float *>(workspace) : nullptr;
     p.n_bh = n_bh;
-    p.n_text = n_text;
-    p.grid_w = grid_w;
-    p.n_tokens = (long long)n_text + (long long)grid_h * grid_w;
+    p.n_text = (unsigned)n_text;
+    p.grid_w = (unsigned)grid_w;
+    p.n_tokens = (unsigned)(n_text + (long long)grid_h * grid_w);
     p.eps = eps;
     p.factor[0] = q_factor;
     p.factor[1] = 1.f;

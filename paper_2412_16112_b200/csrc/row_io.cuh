@@ -117,6 +117,22 @@ struct Pack {
     }
 };
 
+// Asynchronous copy of BYTES (4, 8 or 16) into shared memory.
+template <int BYTES>
+__device__ __forceinline__ void copy_async(uint32_t dst, const void *src)
+{
+    if constexpr (BYTES == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+    else asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" ::"r"(dst), "l"(src), "n"(BYTES) : "memory");
+}
+__device__ __forceinline__ void copies_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+// Until at most LEFT of the thread's latest groups are on their way.
+template <int LEFT>
+__device__ __forceinline__ void copies_wait()
+{
+    if constexpr (LEFT == 0) asm volatile("cp.async.wait_all;" ::: "memory");
+    else asm volatile("cp.async.wait_group %0;" ::"n"(LEFT) : "memory");
+}
+
 __device__ __forceinline__ float warp_sum(float x)
 {
 #pragma unroll

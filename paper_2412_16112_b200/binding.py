@@ -265,29 +265,52 @@ def clear_qk_norm_rope(q, k, q_out, k_out, grid_h, grid_w, n_text, axes_dim, gai
     return q_out, k_out
 
 
-def _on_device_of(t, stream, call):
-    """``call(stream pointer)`` with the device of ``t`` current; its current stream unless one is given."""
+def _launch(fn_name, device, stream, args):
+    """Calls ``fn_name(*args, stream)`` with the device of that number current; on its current stream unless one is given."""
     import torch
-    index = t.device.index
-    if index != torch.cuda.current_device():
-        with torch.cuda.device(index):
-            return _on_device_of(t, stream, call)
-    return call(torch._C._cuda_getCurrentRawStream(index) if stream is None else _stream_ptr(stream))
+    if device != torch.cuda.current_device():
+        with torch.cuda.device(device):
+            return _launch(fn_name, device, stream, args)
+    st = torch._C._cuda_getCurrentRawStream(device) if stream is None else _stream_ptr(stream)
+    status = getattr(_lib or load(), fn_name)(*args, st)
+    if status != OK:
+        raise ClearError(status, fn_name)
+
+
+def _launch_with_workspace(fn_name, device, stream, args, n_bytes):
+    """The same with a workspace and its size before the stream."""
+    import torch
+    if device != torch.cuda.current_device():
+        with torch.cuda.device(device):
+            return _launch_with_workspace(fn_name, device, stream, args, n_bytes)
+    st = torch._C._cuda_getCurrentRawStream(device) if stream is None else _stream_ptr(stream)
+    ws = _workspace(n_bytes, device, st) if n_bytes else None
+    status = getattr(_lib or load(), fn_name)(*args, None if ws is None else ws.data_ptr(), n_bytes, st)
+    if status != OK:
+        raise ClearError(status, fn_name)
 
 
 def _workspace(n_bytes, device, stream_ptr):
     """Device memory for one call on that stream: torch's allocator keeps it from other streams until the call has ended."""
     import torch
-    if stream_ptr == torch._C._cuda_getCurrentRawStream(device.index):
-        return torch.empty(n_bytes, dtype=torch.uint8, device=device)
+    if stream_ptr == torch._C._cuda_getCurrentRawStream(device):
+        return torch.empty(n_bytes, dtype=torch.uint8, device=_cuda(device))
     with torch.cuda.stream(torch.cuda.ExternalStream(stream_ptr, device=device)):
-        return torch.empty(n_bytes, dtype=torch.uint8, device=device)
+        return torch.empty(n_bytes, dtype=torch.uint8, device=_cuda(device))
+
+
+@functools.lru_cache(maxsize=64)
+def _cuda(index):
+    import torch
+    return torch.device("cuda", index)
 
 
 @functools.lru_cache(maxsize=256)
-def _workspace_bytes(fn_name, device_index, *shape):
+def _workspace_bytes(fn_name, device, *shape):
+    import torch
     out = ctypes.c_size_t()
-    _check(getattr(load(), fn_name)(*shape, ctypes.byref(out)), fn_name)
+    with torch.cuda.device(device):
+        _check(getattr(load(), fn_name)(*shape, ctypes.byref(out)), fn_name)
     return out.value
 
 
@@ -300,29 +323,24 @@ def clear_qk_norm_rope_bwd(q, k, dq_rot, dk_rot, dq, dk, grid_h, grid_w, n_text,
     """Gradient of ``clear_qk_norm_rope``: from its inputs ``q``, ``k`` and the gradients ``dq_rot``, ``dk_rot`` of its outputs into
     ``dq``, ``dk`` and, where given, the gains' ``dgain_q``, ``dgain_k`` (fp32, head_dim values).  Returns the four."""
     import torch
-    dtype, shape, device = q.dtype, q.shape, q.device
+    dtype, shape, device = q.dtype, q.shape, q.get_device()
     for t in (q, k, dq_rot, dk_rot, dq, dk):
-        if not (t.is_cuda and t.is_contiguous() and t.dtype == dtype and t.shape == shape and t.device == device):
+        if t.dtype is not dtype or t.get_device() != device or not t.is_contiguous() or t.shape != shape:
             raise ValueError("q, k and the gradients must be contiguous CUDA tensors of one dtype, device and [B, H, N, d] shape")
-    if dtype not in (torch.bfloat16, torch.float32):
-        raise ValueError("bf16 or fp32 tensors")
+    if (dtype is not torch.bfloat16 and dtype is not torch.float32) or device < 0:
+        raise ValueError("bf16 or fp32 CUDA tensors")
     if len(shape) != 4 or shape[2] != n_text + grid_h * grid_w:
         raise ValueError("q must be [B, H, n_text + grid_h * grid_w, d]")
     B, H, _, d = shape
     for g in (gain_q, gain_k, dgain_q, dgain_k):
-        if g is not None and not (g.is_contiguous() and g.dtype == torch.float32 and g.numel() == d and g.device == device):
+        if g is not None and not (g.dtype is torch.float32 and g.numel() == d and g.get_device() == device and g.is_contiguous()):
             raise ValueError("a gain and its gradient are contiguous fp32 tensors of head_dim values on the device of q")
     a0, a1, a2 = axes_dim
-
-    def call(st):
-        n_bytes = 0 if dgain_q is None and dgain_k is None else _workspace_bytes("clear_qk_norm_rope_bwd_workspace", device.index, d)
-        ws = _workspace(n_bytes, device, st) if n_bytes else None
-        _check(load().clear_qk_norm_rope_bwd(q.data_ptr(), k.data_ptr(), dq_rot.data_ptr(), dk_rot.data_ptr(), dq.data_ptr(),
-                                             dk.data_ptr(), _ptr(gain_q), _ptr(gain_k), _ptr(dgain_q), _ptr(dgain_k), B, H, grid_h,
-                                             grid_w, n_text, d, BF16 if dtype == torch.bfloat16 else F32, a0, a1, a2, theta,
-                                             ntk_factor, eps, q_factor, _ptr(ws), n_bytes, st), "clear_qk_norm_rope_bwd")
-
-    _on_device_of(q, stream, call)
+    n_bytes = 0 if dgain_q is None and dgain_k is None else _workspace_bytes("clear_qk_norm_rope_bwd_workspace", device, d)
+    _launch_with_workspace("clear_qk_norm_rope_bwd", device, stream, (
+        q.data_ptr(), k.data_ptr(), dq_rot.data_ptr(), dk_rot.data_ptr(), dq.data_ptr(), dk.data_ptr(), _ptr(gain_q), _ptr(gain_k),
+        _ptr(dgain_q), _ptr(dgain_k), B, H, grid_h, grid_w, n_text, d, BF16 if dtype is torch.bfloat16 else F32, a0, a1, a2, theta,
+        ntk_factor, eps, q_factor), n_bytes)
     return dq, dk, dgain_q, dgain_k
 
 
@@ -344,43 +362,48 @@ def _int_array(values):
 
 def _rope(fn_name, q, k, q_out, k_out, positions, frequencies, axes_dim, layout, factor, stream):
     import torch
-    dtype, shape, device = q.dtype, q.shape, q.device
-    if dtype not in (torch.bfloat16, torch.float32) or not q.is_cuda or len(shape) != 4:
+    dtype, shape, device = q.dtype, q.shape, q.get_device()
+    if (dtype is not torch.bfloat16 and dtype is not torch.float32) or device < 0 or len(shape) != 4:
         raise ValueError("q must be a bf16 or fp32 CUDA tensor [B, H, N, d]")
-    if (k is None) != (k_out is None):
-        raise ValueError("k and k_out come together")
     B, H, N, d = shape
+    Hk = 0
+    if k is None or k_out is None:
+        if k is not k_out:
+            raise ValueError("k and k_out come together")
+        tensors = (q, q_out)
+    else:
+        if len(k.shape) != 4:
+            raise ValueError("k must be [B, Hk, N, d]")
+        Hk = k.shape[1]
+        if k.shape != (B, Hk, N, d) or k_out.shape != k.shape:
+            raise ValueError("k, k_out must share one [B, Hk, N, d] shape, B, N and d being those of q")
+        tensors = (q, q_out, k, k_out)
+    if q_out.shape != shape:
+        raise ValueError("q, q_out must share one [B, H, N, d] shape")
     strides = []
-    for t, t_out in ((q, q_out), (k, k_out)) if k is not None else ((q, q_out),):
-        if t.shape != t_out.shape or t.dim() != 4 or t.shape[0] != B or t.shape[2] != N or t.shape[3] != d:
-            raise ValueError("q, q_out must share one [B, H, N, d] shape, k, k_out one [B, Hk, N, d] shape")
-        for u in (t, t_out):
-            if u.dtype != dtype or u.device != device:
-                raise ValueError("q, k and the outputs must have one dtype and device")
-            sb, sh, sn, sc = u.stride()
-            if sc != 1 and d > 1:
-                raise ValueError("the channels of a head must be contiguous")
-            strides += (sb, sh, sn)
+    for t in tensors:
+        if t.dtype is not dtype or t.get_device() != device:
+            raise ValueError("q, k and the outputs must have one dtype and device")
+        s = t.stride()
+        if s[3] != 1 and d > 1:
+            raise ValueError("the channels of a head must be contiguous")
+        strides += s[:3]
     axes_dim = tuple(axes_dim)
-    if positions.dtype not in (torch.int32, torch.int64) or positions.device != device or positions.dim() != 3 \
-            or positions.shape[0] not in (1, B) or positions.shape[1] != N or positions.shape[2] != len(axes_dim):
+    ps = positions.shape
+    if positions.get_device() != device or len(ps) != 3 or (ps[0] != 1 and ps[0] != B) or ps[1] != N or ps[2] != len(axes_dim) \
+            or (positions.dtype is not torch.int32 and positions.dtype is not torch.int64):
         raise ValueError("positions must be int32 or int64 [B or 1, N, axes] on the device of q")
     pb, pn, pa = positions.stride()
-    if pa != 1 and len(axes_dim) > 1:
+    if pa != 1 and ps[2] > 1:
         raise ValueError("the axes of a position must be contiguous")
-    if frequencies.dtype != torch.float64 or frequencies.is_cuda or not frequencies.is_contiguous() \
+    if frequencies.dtype is not torch.float64 or frequencies.get_device() >= 0 or not frequencies.is_contiguous() \
             or 2 * frequencies.numel() != sum(axes_dim):
         raise ValueError("frequencies must be a contiguous float64 CPU tensor of sum(axes_dim) / 2 values")
-
-    def call(st):
-        _check(getattr(load(), fn_name)(
-            q.data_ptr(), _ptr(k), q_out.data_ptr(), _ptr(k_out), (ctypes.c_longlong * len(strides))(*strides), positions.data_ptr(),
-            0 if positions.shape[0] == 1 else pb, pn, 32 if positions.dtype == torch.int32 else 64, frequencies.data_ptr(),
-            _int_array(axes_dim), len(axes_dim), B, H, 0 if k is None else k.shape[1], N, d,
-            BF16 if dtype == torch.bfloat16 else F32, layout, factor, st), fn_name)
-
-    _on_device_of(q, stream, call)
-    return (q_out, k_out) if k is not None else q_out
+    _launch(fn_name, device, stream, (
+        q.data_ptr(), _ptr(k), q_out.data_ptr(), _ptr(k_out), (ctypes.c_longlong * len(strides))(*strides), positions.data_ptr(),
+        0 if ps[0] == 1 else pb, pn, 32 if positions.dtype is torch.int32 else 64, frequencies.data_ptr(), _int_array(axes_dim),
+        len(axes_dim), B, H, Hk, N, d, BF16 if dtype is torch.bfloat16 else F32, layout, factor))
+    return q_out if k is None else (q_out, k_out)
 
 
 def clear_rope_fwd(q, k, q_out, k_out, positions, frequencies, axes_dim, layout=ROPE_INTERLEAVED, factor=1.0, stream=None):
@@ -397,23 +420,25 @@ def clear_rope_bwd(dq_rot, dk_rot, dq, dk, positions, frequencies, axes_dim, lay
 
 
 def _norm_rows(x, *others):
-    """(B, N, C) and the (batch entry, row) strides of tensors [N, C] or [B, N, C] that share x's shape, dtype and device."""
+    """(B, N, C), the dtype's code, the device's number and the (batch entry, row) strides of tensors [N, C] or [B, N, C] that share
+    x's shape, dtype and device."""
     import torch
-    shape, dtype, device = x.shape, x.dtype, x.device
-    if dtype not in (torch.bfloat16, torch.float32) or not x.is_cuda or len(shape) not in (2, 3):
+    shape, dtype, device = x.shape, x.dtype, x.get_device()
+    dims = len(shape)
+    if (dtype is not torch.bfloat16 and dtype is not torch.float32) or device < 0 or (dims != 3 and dims != 2):
         raise ValueError("x must be a bf16 or fp32 CUDA tensor [N, C] or [B, N, C]")
     strides = []
     for t in (x, *others):
-        if t.shape != shape or t.dtype != dtype or t.device != device:
+        if t.dtype is not dtype or t.get_device() != device or t.shape != shape:
             raise ValueError("x, y and the gradients of rows must share one shape, dtype and device")
         s = t.stride()
         if s[-1] != 1 and shape[-1] > 1:
             raise ValueError("the channels of a row must be contiguous")
-        strides += (0, s[0]) if len(shape) == 2 else (s[0], s[1])
-    return ((1, *shape) if len(shape) == 2 else tuple(shape)), strides
+        strides += s[:2] if dims == 3 else (0, s[0])
+    return shape if dims == 3 else (1, *shape), (BF16 if dtype is torch.bfloat16 else F32), device, strides
 
 
-def _norm_params(x, B, C, *params):
+def _norm_params(x, device, B, C, *params):
     """(dtype code, strides) of weights and biases [C] or [B, C]; None stands for none."""
     import torch
     kind, strides = None, []
@@ -421,21 +446,28 @@ def _norm_params(x, B, C, *params):
         if p is None:
             strides.append(0)
             continue
-        if p.device != x.device or (p.dtype != torch.float32 and p.dtype != x.dtype) or (kind is not None and p.dtype != kind):
-            raise ValueError("weight, bias and their gradients must have one dtype, fp32 or that of x, and the device of x")
-        if p.dim() not in (1, 2) or p.shape[-1] != C or (p.dim() == 2 and p.shape[0] != B):
+        if kind is None:
+            kind = p.dtype
+            if kind is not torch.float32 and kind is not x.dtype:
+                raise ValueError("weight, bias and their gradients must be fp32 or of the dtype of x")
+        if p.dtype is not kind or p.get_device() != device:
+            raise ValueError("weight, bias and their gradients must have one dtype and the device of x")
+        s, shape = p.stride(), p.shape
+        if len(s) == 1 and shape[0] == C:
+            strides.append(0)
+        elif len(s) == 2 and shape[0] == B and shape[1] == C:
+            strides.append(s[0])
+        else:
             raise ValueError("weight, bias and their gradients must be [C] or [B, C]")
-        if p.stride(-1) != 1 and C > 1:
+        if s[-1] != 1 and C > 1:
             raise ValueError("the channels of a weight or bias must be contiguous")
-        kind = p.dtype
-        strides.append(p.stride(0) if p.dim() == 2 else 0)
-    return (BF16 if kind == torch.bfloat16 else F32), strides
+    return (BF16 if kind is torch.bfloat16 else F32), strides
 
 
-def _norm_stats(x, B, N, *stats):
+def _norm_stats(device, n, *stats):
     import torch
     for t in stats:
-        if t is not None and not (t.device == x.device and t.dtype == torch.float32 and t.is_contiguous() and t.numel() == B * N):
+        if t is not None and not (t.dtype is torch.float32 and t.get_device() == device and t.numel() == n and t.is_contiguous()):
             raise ValueError("mean and rstd must be contiguous fp32 tensors of a value a row on the device of x")
 
 
@@ -443,13 +475,12 @@ def clear_layer_norm_fwd(x, y, weight=None, bias=None, mean=None, rstd=None, wei
     """Layer normalisation of the rows of ``x`` ([N, C] or [B, N, C], bf16 or fp32, contiguous channels) into ``y`` (may be ``x``):
     (x - mean) * rstd * (weight_offset + weight) + bias, with weight and bias [C], or [B, C] for a pair a batch entry (a modulated
     layer: ``weight`` the scale, ``weight_offset`` 1, ``bias`` the shift).  ``mean``, ``rstd``: fp32, written for the backward pass."""
-    import torch
-    (B, N, C), strides = _norm_rows(x, y)
-    kind, wb = _norm_params(x, B, C, weight, bias)
-    _norm_stats(x, B, N, mean, rstd)
-    _on_device_of(x, stream, lambda st: _check(load().clear_layer_norm_fwd(
-        x.data_ptr(), y.data_ptr(), _ptr(weight), _ptr(bias), _ptr(mean), _ptr(rstd), B, N, C,
-        BF16 if x.dtype == torch.bfloat16 else F32, kind, *strides, *wb, weight_offset, eps, st), "clear_layer_norm_fwd"))
+    (B, N, C), dtype, device, strides = _norm_rows(x, y)
+    kind, wb = _norm_params(x, device, B, C, weight, bias)
+    _norm_stats(device, B * N, mean, rstd)
+    _launch("clear_layer_norm_fwd", device, stream, (
+        x.data_ptr(), y.data_ptr(), _ptr(weight), _ptr(bias), _ptr(mean), _ptr(rstd), B, N, C, dtype, kind, *strides, *wb,
+        weight_offset, eps))
     return y
 
 
@@ -457,26 +488,22 @@ def clear_layer_norm_bwd(x, dy, weight, mean, rstd, dx, dweight=None, dbias=None
     """Gradient of ``clear_layer_norm_fwd`` from its input, its statistics and the gradient ``dy`` of its output: ``dx`` (may be ``x``
     or ``dy``) and, where given, ``dweight`` and ``dbias``, summed over all rows ([C]) or those of each batch entry ([B, C], as the
     weight is).  Returns the three."""
-    import torch
-    (B, N, C), strides = _norm_rows(x, dy, dx)
-    kind, sums = _norm_params(x, B, C, weight, dweight, dbias)
-    _norm_stats(x, B, N, mean, rstd)
-    forms = {p.dim() for p in (weight, dweight, dbias) if p is not None}
-    if len(forms) > 1:
-        raise ValueError("weight, dweight and dbias must all be [C] or all be [B, C]")
-    per_batch = 1 if forms == {2} else 0
-    device = x.device
-
-    def call(st):
-        n_bytes = 0 if dweight is None and dbias is None else _workspace_bytes("clear_layer_norm_bwd_workspace", device.index, B, N, C,
-                                                                              per_batch)
-        ws = _workspace(n_bytes, device, st) if n_bytes else None
-        _check(load().clear_layer_norm_bwd(
-            x.data_ptr(), dy.data_ptr(), _ptr(weight), mean.data_ptr(), rstd.data_ptr(), dx.data_ptr(), _ptr(dweight), _ptr(dbias),
-            B, N, C, BF16 if x.dtype == torch.bfloat16 else F32, kind, per_batch, *strides, *sums, weight_offset, _ptr(ws), n_bytes,
-            st), "clear_layer_norm_bwd")
-
-    _on_device_of(x, stream, call)
+    (B, N, C), dtype, device, strides = _norm_rows(x, dy, dx)
+    kind, sums = _norm_params(x, device, B, C, weight, dweight, dbias)
+    _norm_stats(device, B * N, mean, rstd)
+    per_batch = None
+    for p in (weight, dweight, dbias):
+        if p is not None:
+            if per_batch is not None and per_batch != p.dim() - 1:
+                raise ValueError("weight, dweight and dbias must all be [C] or all be [B, C]")
+            per_batch = p.dim() - 1
+    per_batch = per_batch or 0
+    n_bytes = 0
+    if dweight is not None or dbias is not None:
+        n_bytes = _workspace_bytes("clear_layer_norm_bwd_workspace", device, B, N, C, per_batch)
+    _launch_with_workspace("clear_layer_norm_bwd", device, stream, (
+        x.data_ptr(), dy.data_ptr(), _ptr(weight), mean.data_ptr(), rstd.data_ptr(), dx.data_ptr(), _ptr(dweight), _ptr(dbias), B, N, C,
+        dtype, kind, per_batch, *strides, *sums, weight_offset), n_bytes)
     return dx, dweight, dbias
 
 

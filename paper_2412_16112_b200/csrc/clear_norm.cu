@@ -12,6 +12,7 @@
 #include <type_traits>
 
 #include "clear_internal.hpp"
+#include "launch_once.hpp"
 #include "ptx.cuh"
 #include "row_io.cuh"
 
@@ -627,15 +628,11 @@ clear_norm_reduce_kernel(const float *partial, int parts, int C, TP *dweight, TP
     }
 }
 
-// ---- launches --------------------------------------------------------------------------------------------------------
+struct Gpu {
+    int device = 0, n_sm = 0;
+};
 
-int sm_count(int *n)
-{
-    int dev = 0;
-    CLEAR_CUDA_TRY(cudaGetDevice(&dev));
-    CLEAR_CUDA_TRY(cudaDeviceGetAttribute(n, cudaDevAttrMultiProcessorCount, dev));
-    return CLEAR_OK;
-}
+// ---- launches --------------------------------------------------------------------------------------------------------
 
 // Accesses of V channels are possible where every row of every tensor begins on their boundary.
 bool vector_fits(const NormArgs &a, int V, size_t elem, size_t param_elem)
@@ -694,32 +691,32 @@ unsigned shares_of(const NormParams &p, int groups, long long resident)
 constexpr int kRowBytesAhead = 36 * 1024;
 
 template <typename T, typename TP, int V, int VPT, int LANES, int WARPS>
-int launch_fwd(NormParams p, int n_sm, cudaStream_t stream)
+int launch_fwd(NormParams p, const Gpu &gpu, cudaStream_t stream)
 {
     constexpr int kThreads = kNormThreads<WARPS>;
     auto kernel = clear_norm_fwd_kernel<T, TP, V, VPT, LANES, WARPS>;
-    const int smem = 2 * (int)sizeof(float) * V * VPT * LANES * WARPS;
-    p.n_vec = p.C / V;
-    if (smem > 32 * 1024) CLEAR_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
+    constexpr int smem = 2 * (int)sizeof(float) * V * VPT * LANES * WARPS;
+    static std::atomic<int> known[kMaxDevices];
     int per_sm = 0;
-    CLEAR_CUDA_TRY(cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per_sm, kernel, kThreads, smem));
+    if (const int rc = kernel_once(known, kernel, kThreads, smem, gpu.device, &per_sm)) return rc;
+    p.n_vec = p.C / V;
     constexpr int kGroups = kThreads / (LANES * WARPS);
     per_sm = std::min(per_sm, std::max(WARPS >= 4 ? 3 : 2, kRowBytesAhead / (kGroups * p.C * (int)sizeof(T))));
-    kernel<<<dim3((unsigned)p.entries, shares_of(p, kGroups, (long long)n_sm * per_sm)), kThreads, smem, stream>>>(p);
+    kernel<<<dim3((unsigned)p.entries, shares_of(p, kGroups, (long long)gpu.n_sm * per_sm)), kThreads, smem, stream>>>(p);
     CLEAR_CUDA_TRY(cudaGetLastError());
     return CLEAR_OK;
 }
 
 // Accesses of one or two channels, 16 channels a thread; UNSUPPORTED above 8192 channels.
 template <typename T, typename TP, int V>
-int narrow_fwd(const NormParams &p, int n_sm, cudaStream_t stream)
+int narrow_fwd(const NormParams &p, const Gpu &gpu, cudaStream_t stream)
 {
-    if (p.C <= 128) return launch_fwd<T, TP, V, 4 / V, 32, 1>(p, n_sm, stream);
-    if (p.C <= 512) return launch_fwd<T, TP, V, 16 / V, 32, 1>(p, n_sm, stream);
-    if (p.C <= 1024) return launch_fwd<T, TP, V, 16 / V, 32, 2>(p, n_sm, stream);
-    if (p.C <= 2048) return launch_fwd<T, TP, V, 16 / V, 32, 4>(p, n_sm, stream);
-    if (p.C <= 4096) return launch_fwd<T, TP, V, 16 / V, 32, 8>(p, n_sm, stream);
-    if (p.C <= 8192) return launch_fwd<T, TP, V, 16 / V, 32, 16>(p, n_sm, stream);
+    if (p.C <= 128) return launch_fwd<T, TP, V, 4 / V, 32, 1>(p, gpu, stream);
+    if (p.C <= 512) return launch_fwd<T, TP, V, 16 / V, 32, 1>(p, gpu, stream);
+    if (p.C <= 1024) return launch_fwd<T, TP, V, 16 / V, 32, 2>(p, gpu, stream);
+    if (p.C <= 2048) return launch_fwd<T, TP, V, 16 / V, 32, 4>(p, gpu, stream);
+    if (p.C <= 4096) return launch_fwd<T, TP, V, 16 / V, 32, 8>(p, gpu, stream);
+    if (p.C <= 8192) return launch_fwd<T, TP, V, 16 / V, 32, 16>(p, gpu, stream);
     return CLEAR_ERR_UNSUPPORTED;
 }
 
@@ -727,32 +724,32 @@ template <typename T, typename TP>
 int norm_fwd(const NormArgs &a, cudaStream_t stream)
 {
     constexpr int kWide = 16 / (int)sizeof(T);
-    int n_sm = 0;
-    if (const int rc = sm_count(&n_sm)) return rc;
+    Gpu gpu;
+    if (const int rc = current_sms(&gpu.device, &gpu.n_sm)) return rc;
     NormParams p = params_of(a, a.w_stride_b || a.bias_stride_b);
     if (vector_fits(a, kWide, sizeof(T), sizeof(TP))) {
         // up to four accesses of 16 bytes a thread, then more warps
         const int n = (a.C / kWide + 31) / 32;  // accesses, in warps
-        if (a.C / kWide <= 8) return launch_fwd<T, TP, kWide, 1, 8, 1>(p, n_sm, stream);
-        if (a.C / kWide <= 16) return launch_fwd<T, TP, kWide, 2, 8, 1>(p, n_sm, stream);
-        if (n <= 1) return launch_fwd<T, TP, kWide, 4, 8, 1>(p, n_sm, stream);
-        if (n <= 2) return launch_fwd<T, TP, kWide, 4, 16, 1>(p, n_sm, stream);
-        if (n <= 3) return launch_fwd<T, TP, kWide, 3, 32, 1>(p, n_sm, stream);
-        if (n <= 4) return launch_fwd<T, TP, kWide, 4, 32, 1>(p, n_sm, stream);
-        if (n <= 6) return launch_fwd<T, TP, kWide, 3, 32, 2>(p, n_sm, stream);
-        if (n <= 8) return launch_fwd<T, TP, kWide, 4, 32, 2>(p, n_sm, stream);
-        if (n <= 12) return launch_fwd<T, TP, kWide, 3, 32, 4>(p, n_sm, stream);
-        if (n <= 16) return launch_fwd<T, TP, kWide, 4, 32, 4>(p, n_sm, stream);
-        if (n <= 24) return launch_fwd<T, TP, kWide, 3, 32, 8>(p, n_sm, stream);
-        if (n <= 32) return launch_fwd<T, TP, kWide, 4, 32, 8>(p, n_sm, stream);
-        if (n <= 48) return launch_fwd<T, TP, kWide, 3, 32, 16>(p, n_sm, stream);
-        if (n <= 64) return launch_fwd<T, TP, kWide, 4, 32, 16>(p, n_sm, stream);
+        if (a.C / kWide <= 8) return launch_fwd<T, TP, kWide, 1, 8, 1>(p, gpu, stream);
+        if (a.C / kWide <= 16) return launch_fwd<T, TP, kWide, 2, 8, 1>(p, gpu, stream);
+        if (n <= 1) return launch_fwd<T, TP, kWide, 4, 8, 1>(p, gpu, stream);
+        if (n <= 2) return launch_fwd<T, TP, kWide, 4, 16, 1>(p, gpu, stream);
+        if (n <= 3) return launch_fwd<T, TP, kWide, 3, 32, 1>(p, gpu, stream);
+        if (n <= 4) return launch_fwd<T, TP, kWide, 4, 32, 1>(p, gpu, stream);
+        if (n <= 6) return launch_fwd<T, TP, kWide, 3, 32, 2>(p, gpu, stream);
+        if (n <= 8) return launch_fwd<T, TP, kWide, 4, 32, 2>(p, gpu, stream);
+        if (n <= 12) return launch_fwd<T, TP, kWide, 3, 32, 4>(p, gpu, stream);
+        if (n <= 16) return launch_fwd<T, TP, kWide, 4, 32, 4>(p, gpu, stream);
+        if (n <= 24) return launch_fwd<T, TP, kWide, 3, 32, 8>(p, gpu, stream);
+        if (n <= 32) return launch_fwd<T, TP, kWide, 4, 32, 8>(p, gpu, stream);
+        if (n <= 48) return launch_fwd<T, TP, kWide, 3, 32, 16>(p, gpu, stream);
+        if (n <= 64) return launch_fwd<T, TP, kWide, 4, 32, 16>(p, gpu, stream);
     } else if (vector_fits(a, 2, sizeof(T), sizeof(TP))) {
-        if (const int rc = narrow_fwd<T, TP, 2>(p, n_sm, stream); rc != CLEAR_ERR_UNSUPPORTED) return rc;
-    } else if (const int rc = narrow_fwd<T, TP, 1>(p, n_sm, stream); rc != CLEAR_ERR_UNSUPPORTED) {
+        if (const int rc = narrow_fwd<T, TP, 2>(p, gpu, stream); rc != CLEAR_ERR_UNSUPPORTED) return rc;
+    } else if (const int rc = narrow_fwd<T, TP, 1>(p, gpu, stream); rc != CLEAR_ERR_UNSUPPORTED) {
         return rc;
     }
-    clear_norm_fwd_long_kernel<T, TP><<<dim3((unsigned)p.entries, shares_of(p, 1, 8LL * n_sm)), 256, 0, stream>>>(p);
+    clear_norm_fwd_long_kernel<T, TP><<<dim3((unsigned)p.entries, shares_of(p, 1, 8LL * gpu.n_sm)), 256, 0, stream>>>(p);
     CLEAR_CUDA_TRY(cudaGetLastError());
     return CLEAR_OK;
 }
@@ -776,18 +773,21 @@ int launch_reduce(const NormArgs &a, int parts, cudaStream_t stream)
 }
 
 template <typename T, typename TP, int V, int VPT, int LANES, int WARPS>
-int launch_bwd(NormParams p, const NormArgs &a, int n_sm, cudaStream_t stream)
+int launch_bwd(NormParams p, const NormArgs &a, const Gpu &gpu, cudaStream_t stream)
 {
     constexpr int kThreads = kBwdThreads<T, V, LANES, WARPS>;
     auto kernel = clear_norm_bwd_kernel<T, TP, V, VPT, LANES, WARPS>;
     const bool sums = a.dweight || a.dbias;
-    const unsigned shares = shares_of(p, kBwdGroups<T, V, LANES, WARPS> * kRowsAtOnce<V, VPT>, n_sm);
+    const unsigned shares = shares_of(p, kBwdGroups<T, V, LANES, WARPS> * kRowsAtOnce<V, VPT>, gpu.n_sm);
     p.n_vec = p.C / V;
     p.partial = sums ? static_cast<float *>(a.workspace) : nullptr;
-    const int terms = LANES < 32 ? kThreads / 32 : kBwdGroups<T, V, LANES, WARPS>;
+    constexpr int terms = LANES < 32 ? kThreads / 32 : kBwdGroups<T, V, LANES, WARPS>;
     constexpr int ring = kBwdStages<T, V, VPT, LANES, WARPS> * kBwdStep<T, V, VPT, LANES, WARPS>;
     const int smem = std::max(ring, sums ? terms * 2 * (int)sizeof(float) * p.C : 0);
-    if (smem > 32 * 1024) CLEAR_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
+    constexpr int most = std::max(ring, terms * 2 * (int)sizeof(float) * LANES * WARPS * V * VPT);
+    static std::atomic<int> known[kMaxDevices];
+    int per_sm = 0;
+    if (const int rc = kernel_once(known, kernel, kThreads, most, gpu.device, &per_sm)) return rc;
     kernel<<<dim3((unsigned)p.entries, shares), kThreads, smem, stream>>>(p);
     CLEAR_CUDA_TRY(cudaGetLastError());
     return sums ? launch_reduce<TP>(a, a.per_batch ? shares : shares * p.entries, stream) : CLEAR_OK;
@@ -795,14 +795,14 @@ int launch_bwd(NormParams p, const NormArgs &a, int n_sm, cudaStream_t stream)
 
 // Accesses of one or two channels; UNSUPPORTED above 8192 channels.
 template <typename T, typename TP, int V>
-int narrow_bwd(const NormParams &p, const NormArgs &a, int n_sm, cudaStream_t stream)
+int narrow_bwd(const NormParams &p, const NormArgs &a, const Gpu &gpu, cudaStream_t stream)
 {
-    if (a.C <= 256) return launch_bwd<T, TP, V, 8 / V, 32, 1>(p, a, n_sm, stream);
-    if (a.C <= 512) return launch_bwd<T, TP, V, 8 / V, 32, 2>(p, a, n_sm, stream);
-    if (a.C <= 1024) return launch_bwd<T, TP, V, 8 / V, 32, 4>(p, a, n_sm, stream);
-    if (a.C <= 2048) return launch_bwd<T, TP, V, 8 / V, 32, 8>(p, a, n_sm, stream);
-    if (a.C <= 4096) return launch_bwd<T, TP, V, 8 / V, 32, 16>(p, a, n_sm, stream);
-    if (a.C <= 8192) return launch_bwd<T, TP, V, 16 / V, 32, 16>(p, a, n_sm, stream);
+    if (a.C <= 256) return launch_bwd<T, TP, V, 8 / V, 32, 1>(p, a, gpu, stream);
+    if (a.C <= 512) return launch_bwd<T, TP, V, 8 / V, 32, 2>(p, a, gpu, stream);
+    if (a.C <= 1024) return launch_bwd<T, TP, V, 8 / V, 32, 4>(p, a, gpu, stream);
+    if (a.C <= 2048) return launch_bwd<T, TP, V, 8 / V, 32, 8>(p, a, gpu, stream);
+    if (a.C <= 4096) return launch_bwd<T, TP, V, 8 / V, 32, 16>(p, a, gpu, stream);
+    if (a.C <= 8192) return launch_bwd<T, TP, V, 16 / V, 32, 16>(p, a, gpu, stream);
     return CLEAR_ERR_UNSUPPORTED;
 }
 
@@ -810,36 +810,36 @@ template <typename T, typename TP>
 int norm_bwd(const NormArgs &a, cudaStream_t stream)
 {
     constexpr int kWide = 16 / (int)sizeof(T), kUnit = 8 / kWide;  // accesses of 8 channels
-    int n_sm = 0;
-    if (const int rc = sm_count(&n_sm)) return rc;
+    Gpu gpu;
+    if (const int rc = current_sms(&gpu.device, &gpu.n_sm)) return rc;
     NormParams p = params_of(a, a.per_batch);
     if (vector_fits(a, kWide, sizeof(T), sizeof(TP))) {
-        if (a.C <= 64) return launch_bwd<T, TP, kWide, kUnit, 8, 1>(p, a, n_sm, stream);
-        if (a.C <= 128) return launch_bwd<T, TP, kWide, kUnit, 16, 1>(p, a, n_sm, stream);
-        if (a.C <= 256) return launch_bwd<T, TP, kWide, kUnit, 32, 1>(p, a, n_sm, stream);
-        if (a.C <= 512) return launch_bwd<T, TP, kWide, kUnit, 32, 2>(p, a, n_sm, stream);
-        if (a.C <= 768) return launch_bwd<T, TP, kWide, kUnit, 32, 3>(p, a, n_sm, stream);
-        if (a.C <= 1024) return launch_bwd<T, TP, kWide, kUnit, 32, 4>(p, a, n_sm, stream);
-        if (a.C <= 1536) return launch_bwd<T, TP, kWide, kUnit, 32, 6>(p, a, n_sm, stream);
-        if (a.C <= 2048) return launch_bwd<T, TP, kWide, kUnit, 32, 8>(p, a, n_sm, stream);
+        if (a.C <= 64) return launch_bwd<T, TP, kWide, kUnit, 8, 1>(p, a, gpu, stream);
+        if (a.C <= 128) return launch_bwd<T, TP, kWide, kUnit, 16, 1>(p, a, gpu, stream);
+        if (a.C <= 256) return launch_bwd<T, TP, kWide, kUnit, 32, 1>(p, a, gpu, stream);
+        if (a.C <= 512) return launch_bwd<T, TP, kWide, kUnit, 32, 2>(p, a, gpu, stream);
+        if (a.C <= 768) return launch_bwd<T, TP, kWide, kUnit, 32, 3>(p, a, gpu, stream);
+        if (a.C <= 1024) return launch_bwd<T, TP, kWide, kUnit, 32, 4>(p, a, gpu, stream);
+        if (a.C <= 1536) return launch_bwd<T, TP, kWide, kUnit, 32, 6>(p, a, gpu, stream);
+        if (a.C <= 2048) return launch_bwd<T, TP, kWide, kUnit, 32, 8>(p, a, gpu, stream);
         // 16 channels a thread or 16 warps a row: 16896 rows 73 or 88 us in bf16, 139 or 125 in fp32
         if (a.C <= 4096)
-            return sizeof(T) == 2 ? launch_bwd<T, TP, kWide, 2 * kUnit, 32, 8>(p, a, n_sm, stream)
-                                  : launch_bwd<T, TP, kWide, kUnit, 32, 16>(p, a, n_sm, stream);
-        if (a.C <= 8192) return launch_bwd<T, TP, kWide, 2 * kUnit, 32, 16>(p, a, n_sm, stream);
+            return sizeof(T) == 2 ? launch_bwd<T, TP, kWide, 2 * kUnit, 32, 8>(p, a, gpu, stream)
+                                  : launch_bwd<T, TP, kWide, kUnit, 32, 16>(p, a, gpu, stream);
+        if (a.C <= 8192) return launch_bwd<T, TP, kWide, 2 * kUnit, 32, 16>(p, a, gpu, stream);
     } else if (vector_fits(a, 2, sizeof(T), sizeof(TP))) {
-        if (const int rc = narrow_bwd<T, TP, 2>(p, a, n_sm, stream); rc != CLEAR_ERR_UNSUPPORTED) return rc;
-    } else if (const int rc = narrow_bwd<T, TP, 1>(p, a, n_sm, stream); rc != CLEAR_ERR_UNSUPPORTED) {
+        if (const int rc = narrow_bwd<T, TP, 2>(p, a, gpu, stream); rc != CLEAR_ERR_UNSUPPORTED) return rc;
+    } else if (const int rc = narrow_bwd<T, TP, 1>(p, a, gpu, stream); rc != CLEAR_ERR_UNSUPPORTED) {
         return rc;
     }
     if (a.dweight || a.dbias) {
-        const unsigned shares = shares_of(p, 1, n_sm);
+        const unsigned shares = shares_of(p, 1, gpu.n_sm);
         p.partial = static_cast<float *>(a.workspace);
         clear_norm_columns_kernel<T><<<dim3((unsigned)p.entries, shares, (a.C + 255) / 256), 256, 0, stream>>>(p);
         CLEAR_CUDA_TRY(cudaGetLastError());
         if (const int rc = launch_reduce<TP>(a, a.per_batch ? shares : shares * p.entries, stream)) return rc;
     }
-    clear_norm_bwd_long_kernel<T, TP><<<dim3((unsigned)p.entries, shares_of(p, 1, 8LL * n_sm)), 256, 0, stream>>>(p);
+    clear_norm_bwd_long_kernel<T, TP><<<dim3((unsigned)p.entries, shares_of(p, 1, 8LL * gpu.n_sm)), 256, 0, stream>>>(p);
     CLEAR_CUDA_TRY(cudaGetLastError());
     return CLEAR_OK;
 }
@@ -849,9 +849,9 @@ int norm_bwd(const NormArgs &a, cudaStream_t stream)
 // A partial sum of each block: one an SM, or one a batch entry where there are more of those.
 int norm_bwd_workspace(int B, int N, int C, size_t *bytes)
 {
-    int n_sm = 0;
-    if (const int rc = sm_count(&n_sm)) return rc;
-    *bytes = (size_t)std::min<long long>((long long)B * N, std::max(n_sm, B)) * 2 * sizeof(float) * (size_t)C;
+    Gpu gpu;
+    if (const int rc = current_sms(&gpu.device, &gpu.n_sm)) return rc;
+    *bytes = (size_t)std::min<long long>((long long)B * N, std::max(gpu.n_sm, B)) * 2 * sizeof(float) * (size_t)C;
     return CLEAR_OK;
 }
 

@@ -11,6 +11,7 @@
 #include <cmath>
 
 #include "clear_internal.hpp"
+#include "launch_once.hpp"
 #include "ptx.cuh"
 #include "rope_angle.cuh"
 #include "row_io.cuh"
@@ -195,17 +196,8 @@ __global__ void __launch_bounds__(256) clear_prep_gain_kernel(const float *parti
     if (lane == 0 && out) out[col % D] = sum;
 }
 
-int grid_size(int *blocks)
-{
-    int dev = 0, n_sm = 0;
-    CLEAR_CUDA_TRY(cudaGetDevice(&dev));
-    CLEAR_CUDA_TRY(cudaDeviceGetAttribute(&n_sm, cudaDevAttrMultiProcessorCount, dev));
-    *blocks = kBlocksPerSm * n_sm;
-    return CLEAR_OK;
-}
-
 template <typename T, int D>
-int launch(PrepBwdParams &p, float *dgain_q, float *dgain_k, int most, cudaStream_t stream)
+int launch(PrepBwdParams &p, float *dgain_q, float *dgain_k, int device, int most, cudaStream_t stream)
 {
     constexpr int kTokens = 32 / (D / kEpl);
     const int groups = (int)((p.n_tokens + kTokens - 1) / kTokens), warps = most * (kWarps / 2);
@@ -215,7 +207,9 @@ int launch(PrepBwdParams &p, float *dgain_q, float *dgain_k, int most, cudaStrea
     p.parts = (unsigned)((p.n_bh + p.bh_a_part - 1) / p.bh_a_part);
     const int blocks = (int)std::min<long long>(most, ((long long)groups * p.parts + kWarps / 2 - 1) / (kWarps / 2));
     constexpr int smem = kRingBytes<T>;
-    if (smem) CLEAR_CUDA_TRY(cudaFuncSetAttribute(clear_prep_bwd_kernel<T, D>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
+    static std::atomic<int> known[kMaxDevices];
+    int per_sm = 0;
+    if (const int rc = kernel_once(known, clear_prep_bwd_kernel<T, D>, kThreads, smem, device, &per_sm)) return rc;
     clear_prep_bwd_kernel<T, D><<<blocks, kThreads, smem, stream>>>(p);
     CLEAR_CUDA_TRY(cudaGetLastError());
     if (!p.partial) return CLEAR_OK;
@@ -236,9 +230,9 @@ int launch(PrepBwdParams &p, float *dgain_q, float *dgain_k, int most, cudaStrea
 
 int prep_bwd_workspace(int head_dim, size_t *bytes)
 {
-    int blocks = 0;
-    if (const int rc = grid_size(&blocks)) return rc;
-    *bytes = (size_t)blocks * 2 * head_dim * sizeof(float);
+    int device = 0, n_sm = 0;
+    if (const int rc = current_sms(&device, &n_sm)) return rc;
+    *bytes = (size_t)kBlocksPerSm * n_sm * 2 * head_dim * sizeof(float);
     return CLEAR_OK;
 }
 
@@ -247,8 +241,9 @@ int launch_prep_bwd(const void *q, const void *k, const void *dq_rot, const void
                     int dtype, const int axes_dim[3], double theta, double ntk_factor, float eps, float q_factor, void *workspace,
                     cudaStream_t stream)
 {
-    int most = 0;
-    if (const int rc = grid_size(&most)) return rc;
+    int device = 0, n_sm = 0;
+    if (const int rc = current_sms(&device, &n_sm)) return rc;
+    const int most = kBlocksPerSm * n_sm;
     PrepBwdParams p{};
     p.x[0] = q; p.x[1] = k;
     p.dy[0] = dq_rot; p.dy[1] = dk_rot;
@@ -273,10 +268,10 @@ int launch_prep_bwd(const void *q, const void *k, const void *dq_rot, const void
         }
     }
     if (dtype == CLEAR_BF16)
-        return head_dim == 128 ? launch<__nv_bfloat16, 128>(p, dgain_q, dgain_k, most, stream)
-                               : launch<__nv_bfloat16, 64>(p, dgain_q, dgain_k, most, stream);
-    return head_dim == 128 ? launch<float, 128>(p, dgain_q, dgain_k, most, stream)
-                           : launch<float, 64>(p, dgain_q, dgain_k, most, stream);
+        return head_dim == 128 ? launch<__nv_bfloat16, 128>(p, dgain_q, dgain_k, device, most, stream)
+                               : launch<__nv_bfloat16, 64>(p, dgain_q, dgain_k, device, most, stream);
+    return head_dim == 128 ? launch<float, 128>(p, dgain_q, dgain_k, device, most, stream)
+                           : launch<float, 64>(p, dgain_q, dgain_k, device, most, stream);
 }
 
 }  // namespace clear

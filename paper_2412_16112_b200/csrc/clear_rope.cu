@@ -9,6 +9,7 @@
 #include <algorithm>
 
 #include "clear_internal.hpp"
+#include "launch_once.hpp"
 #include "rope_angle.cuh"
 #include "row_io.cuh"
 
@@ -247,9 +248,8 @@ int launch_for(RopeParams &p, const RopeArgs &a, int n_sm, cudaStream_t stream)
 
 int launch_rope(const RopeArgs &a, cudaStream_t stream)
 {
-    int dev = 0, n_sm = 0;
-    CLEAR_CUDA_TRY(cudaGetDevice(&dev));
-    CLEAR_CUDA_TRY(cudaDeviceGetAttribute(&n_sm, cudaDevAttrMultiProcessorCount, dev));
+    int device = 0, n_sm = 0;
+    if (const int rc = current_sms(&device, &n_sm)) return rc;
     RopeParams p{};
     int pair = 0;
     for (int x = 0; x < a.n_axes; ++x)

@@ -292,12 +292,13 @@ int clear_rope_bwd(const void *q, const void *k, void *q_out, void *k_out, const
  * weight, bias: C values each (strides 0), or C values a batch entry (weight_stride_b, bias_stride_b); NULL stands for a gain of one
  * (whatever weight_offset) and a bias of zero.  A modulated layer passes its scale as weight with weight_offset 1, and its shift.
  * x, y: device memory, bf16 or fp32, channels contiguous, strides of the batch entries and rows in elements; y may be x with the same
- * strides, any other overlap is not allowed.  param_dtype: the type of weight and bias, fp32 or that of x.  mean, rstd: [B, N] fp32
- * contiguous, written for the backward pass, or NULL.  fp32 arithmetic, two passes over a row's registers, so an offset common to a
- * row costs no accuracy.  One launch on `stream`, no allocation, no host synchronisation.  B or N of zero: nothing is done.
+ * strides; any other overlap is not allowed, nor are rows of y to overlap.  param_dtype: the type of weight and bias, fp32 or that of
+ * x.  mean, rstd: [B, N] fp32 contiguous, written for the backward pass, or NULL.  fp32 arithmetic; the squares are summed around the
+ * row's mean, so an offset common to a row costs no accuracy.  One launch on `stream`, no allocation, no host synchronisation.  B or N
+ * of zero: nothing is done.
  * Errors: INVALID_ARG (a negative size, C <= 0, a null x or y, unknown types, param_dtype bf16 with fp32 x, eps < 0, a non-finite
  * value, y equal to x under other strides, rows of y that fall on one another by a stride of zero), UNSUPPORTED (2^31 rows or
- * more), MISALIGNED (a pointer that is not a multiple of its element), CUDA. */
+ * more, more than 2^23 channels), MISALIGNED (a pointer that is not a multiple of its element), CUDA. */
 int clear_layer_norm_fwd(const void *x, void *y, const void *weight, const void *bias, float *mean, float *rstd, int B, int N, int C,
                          int dtype, int param_dtype, long long x_stride_b, long long x_stride_n, long long y_stride_b,
                          long long y_stride_n, long long weight_stride_b, long long bias_stride_b, float weight_offset, float eps,

@@ -12,12 +12,15 @@ bool misaligned(const void *p, size_t bytes) { return reinterpret_cast<uintptr_t
 size_t size_of(int dtype) { return dtype == CLEAR_BF16 ? 2 : 4; }
 bool is_dtype(int dtype) { return dtype == CLEAR_BF16 || dtype == CLEAR_F32; }
 
+// Launches' grids hold this many channels with room to spare.
+constexpr int kMaxChannels = 1 << 23;
+
 int check_norm(const NormArgs &a, const void *x, void *out)
 {
     if (a.B < 0 || a.N < 0 || a.C <= 0 || !is_dtype(a.dtype) || !is_dtype(a.param_dtype)) return CLEAR_ERR_INVALID_ARG;
     if (a.dtype == CLEAR_F32 && a.param_dtype != CLEAR_F32) return CLEAR_ERR_INVALID_ARG;
     if (!(a.eps >= 0.f) || !std::isfinite(a.eps) || !std::isfinite(a.offset)) return CLEAR_ERR_INVALID_ARG;
-    if ((long long)a.B * a.N > 0x7fffffffLL) return CLEAR_ERR_UNSUPPORTED;
+    if ((long long)a.B * a.N > 0x7fffffffLL || a.C > kMaxChannels) return CLEAR_ERR_UNSUPPORTED;
     if (a.B == 0 || a.N == 0) return CLEAR_OK;
     if (!x || !out) return CLEAR_ERR_INVALID_ARG;
     // rows of the output that are one and the same
@@ -154,7 +157,7 @@ int clear_layer_norm_fwd(const void *x, void *y, const void *weight, const void 
 int clear_layer_norm_bwd_workspace(int B, int N, int C, int per_batch, size_t *bytes)
 {
     if (!bytes || B < 0 || N < 0 || C <= 0) return CLEAR_ERR_INVALID_ARG;
-    if ((long long)B * N > 0x7fffffffLL || (per_batch && B > 65535)) return CLEAR_ERR_UNSUPPORTED;
+    if ((long long)B * N > 0x7fffffffLL || C > kMaxChannels || (per_batch && B > 65535)) return CLEAR_ERR_UNSUPPORTED;
     *bytes = 0;
     return B == 0 || N == 0 ? CLEAR_OK : norm_bwd_workspace(B, N, C, bytes);
 }

@@ -607,9 +607,9 @@ clear_norm_reduce_kernel(const float *partial, int parts, int C, TP *dweight, TP
 {
     constexpr int kShares = kReduceThreads / kReduceChannels;
     __shared__ float s[kReduceThreads / 32][kReduceChannels];
-    const int sub = threadIdx.x % kReduceChannels, share = threadIdx.x / kReduceChannels, col = blockIdx.y * kReduceChannels + sub;
+    const int sub = threadIdx.x % kReduceChannels, share = threadIdx.x / kReduceChannels, col = blockIdx.x * kReduceChannels + sub;
     TP *out = blockIdx.z == 0 ? dweight : dbias;
-    const float *src = partial + ((size_t)blockIdx.x * parts * 2 + blockIdx.z) * C + col;
+    const float *src = partial + ((size_t)blockIdx.y * parts * 2 + blockIdx.z) * C + col;
     ptx::grid_wait();
     if (!out) return;
     float sum = 0.f;
@@ -624,7 +624,7 @@ clear_norm_reduce_kernel(const float *partial, int parts, int C, TP *dweight, TP
     if (threadIdx.x < kReduceChannels && col < C) {
 #pragma unroll
         for (int i = 1; i < kReduceThreads / 32; ++i) sum += s[i][sub];
-        out[(long long)blockIdx.x * (blockIdx.z == 0 ? dw_stride_b : db_stride_b) + col] = (TP)sum;
+        out[(long long)blockIdx.y * (blockIdx.z == 0 ? dw_stride_b : db_stride_b) + col] = (TP)sum;
     }
 }
 
@@ -762,7 +762,7 @@ int launch_reduce(const NormArgs &a, int parts, cudaStream_t stream)
     cudaLaunchAttribute attr{};
     attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr.val.programmaticStreamSerializationAllowed = 1;
-    cfg.gridDim = dim3(a.per_batch ? a.B : 1, (a.C + kReduceChannels - 1) / kReduceChannels, 2);
+    cfg.gridDim = dim3((a.C + kReduceChannels - 1) / kReduceChannels, a.per_batch ? a.B : 1, 2);
     cfg.blockDim = dim3(kReduceThreads);
     cfg.stream = stream;
     cfg.attrs = &attr;

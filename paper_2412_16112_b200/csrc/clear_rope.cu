@@ -226,7 +226,7 @@ int launch(RopeParams &p, const RopeArgs &a, int n_sm, cudaStream_t stream)
     // share 21.8, four 23.1; 16680 of 24 fp32 heads 43.6, 58.8, 42.9); fewer to a share while SMs would be without work.
     const int heads = p.t[0].heads + p.t[1].heads;
     const int parts = (int)std::min<long long>(heads, std::max<long long>((heads + 7) / 8, 4LL * n_sm / blocks));
-    p.heads_a_part = (heads + parts - 1) / parts;
+    p.heads_a_part = std::max((heads + parts - 1) / parts, (heads + 65534) / 65535);
     const dim3 grid((unsigned)blocks, (unsigned)((heads + p.heads_a_part - 1) / p.heads_a_part));
     if (a.pos64) clear_rope_kernel<T, V, HALF, int64_t><<<grid, kRopeThreads, 0, stream>>>(p);
     else clear_rope_kernel<T, V, HALF, int32_t><<<grid, kRopeThreads, 0, stream>>>(p);

@@ -115,6 +115,35 @@ def test_layer_norm_of_very_long_rows(dtype, C):
     _check_norm(x, dy, w, b, 0.0)
 
 
+@pytest.mark.parametrize("dtype,pdtype", [("bf16", "bf16"), ("bf16", "f32"), ("f32", "f32")])
+@pytest.mark.parametrize("C", [10, 65, 72, 128, 130, 136, 250, 320, 500, 513, 640, 1002, 1030, 1160, 2002, 2049, 3000, 4098, 4101, 6000, 6001,
+                               6002, 8194])
+def test_layer_norm_widths_at_the_kernels_borders(dtype, pdtype, C):
+    """Widths on both sides of where another kernel, another number of warps or another width of access takes over; rows that do not
+    fill the last block."""
+    x, dy, w, b = _norm_inputs(1, 3 + C % 7, C, DTYPES[dtype], DTYPES[pdtype], "shared", C)
+    _check_norm(x, dy, w, b, 0.0)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("C", [10000, 12288, 16384, 16392, 24576])
+def test_layer_norm_wide_rows(dtype, C):
+    x, dy, w, b = _norm_inputs(2, 3, C, DTYPES[dtype], DTYPES[dtype], "batch", C)
+    _check_norm(x, dy, w, b, 1.0)
+
+
+@pytest.mark.parametrize("C", [24, 61, 128, 520])
+@pytest.mark.parametrize("B,N", [(700, 1), (300, 3), (151, 7)])
+def test_layer_norm_more_batch_entries_than_sms(B, N, C):
+    """A block an entry, or, with shared weights, one run of all rows, or entries that lie apart."""
+    x, dy, w, b = _norm_inputs(B, N, C, torch.bfloat16, torch.float32, "batch", B)
+    _check_norm(x, dy, w, b, 1.0)
+    _check_norm(x, dy, w[0].contiguous(), b[0].contiguous(), 0.0)
+    apart = torch.zeros(B, N + 1, C, device="cuda", dtype=torch.bfloat16)
+    apart[:, :N].copy_(x)
+    _check_norm(apart[:, :N], dy, w[0].contiguous(), b[0].contiguous(), 0.0)
+
+
 @pytest.mark.parametrize("B,N", [(1, 1), (1, 2), (3, 1), (1, 37), (2, 300), (5, 61), (300, 2), (1, 5000), (3, 1237)])
 @pytest.mark.parametrize("dtype,C", [("bf16", 96), ("bf16", 50), ("f32", 61), ("f32", 520)])
 @pytest.mark.parametrize("form", ["none", "shared", "batch"])
@@ -209,7 +238,7 @@ def test_layer_norm_statistics_of_rows_far_from_zero():
     assert not y.any()
 
 
-@pytest.mark.parametrize("C", [512, 61, 6000])
+@pytest.mark.parametrize("C", [512, 61, 6000, 32, 256])
 def test_layer_norm_rows_that_are_not_finite_stay_alone(C):
     x, dy, w, b = _norm_inputs(1, 40, C, torch.float32, torch.float32, "shared", 21)
     clean = clear.clear_layer_norm_fwd(x, torch.empty_like(x), w, b)
@@ -376,6 +405,16 @@ def test_rope_strides(dtype, layout, lead):
     assert torch.equal(q, heads[0]) and torch.equal(k, heads[1]) and torch.equal(rows[:, :, H + Hk:], values)
 
 
+@pytest.mark.parametrize("H,Hk,N", [(1, 1, 3), (3, 2, 5), (7, 1, 40), (9, 9, 700), (17, 3, 3000), (40, 8, 2)])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("layout", [clear.ROPE_INTERLEAVED, clear.ROPE_HALF])
+def test_rope_numbers_of_heads(H, Hk, N, dtype, layout):
+    """Shares of heads that end in the middle of a tensor, batches of heads that are not full, part of a head copied."""
+    q, k = _randn((1, H, N, 48), N, DTYPES[dtype]), _randn((1, Hk, N, 48), N + 1, DTYPES[dtype])
+    positions = torch.arange(N, device="cuda", dtype=torch.int32).reshape(1, N, 1)
+    _check_rope(q, k, positions, clear.clear_rope_frequencies(32), (32,), layout, 1.0)
+
+
 def test_rope_one_in_place_and_one_not():
     q, k = _randn((1, 4, 30, 48), 1), _randn((1, 2, 30, 48), 2)
     positions, freqs = torch.arange(30, device="cuda").reshape(1, 30, 1), clear.clear_rope_frequencies(16)
@@ -473,6 +512,24 @@ def _check_prep(B, H, gh, gw, T, d, axes, dtype, gains, ntk, qf, over=None, eps=
 def test_prep_gradient(B, H, gh, gw, T, d, axes, dtype, gains, ntk, qf):
     for over in (None, "x", "dy"):
         _check_prep(B, H, gh, gw, T, d, axes, dtype, gains, ntk, qf, over)
+
+
+@pytest.mark.parametrize("n_bh", [1, 2, 3, 4, 5, 6, 7, 25])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_prep_gradient_numbers_of_rows(n_bh, dtype):
+    """Steps of two or three rows that the rows of a token do not fill, with more tokens than warps and with few."""
+    _check_prep(1, n_bh, 60, 61, 3, 64, (8, 28, 28), dtype, True, 1.0, 1.0)
+    _check_prep(n_bh, 1, 2, 3, 3, 128, (16, 56, 56), dtype, True, 1.0, 1.0, over="dy")
+
+
+def test_prep_gradient_of_small_rows():
+    """Rows of size 1e-12 without eps: inv = 1e12 stays in range through its third power."""
+    q, k, dqr, dkr = (_randn((1, 2, 10, 64), i) for i in range(4))
+    q *= 1e-12
+    args = (3, 3, 1, (8, 28, 28))
+    want = oracle.qk_prep_grad(_np(q), _np(dqr), None, oracle_prep.token_positions(3, 3, 1), args[3], 10000.0, 1.0, 0.0, 1.0)[0]
+    dq = clear.clear_qk_norm_rope_bwd(q, k, dqr, dkr, torch.empty_like(q), torch.empty_like(q), *args, eps=0.0)[0]
+    _close(dq, want, 100 * U * np.abs(want).max(), torch.float32)
 
 
 def test_prep_gradient_without_sums_and_repeats():

@@ -249,3 +249,13 @@ def test_oracle_gradient_of_the_preparation():
 def test_oracle_by_parts_is_continuous_and_ordered():
     a = oracle.frequencies(128, 10000.0, "parts", 8.0, 4096.0)
     assert (np.diff(a) < 0).all() and a[0] == 1.0 and math.isclose(a[-1] * 8, oracle.frequencies(128, 10000.0)[-1])
+
+
+def test_layer_norm_refuses_more_channels_than_its_grids_hold():
+    assert _norm_fwd(C=2 ** 23 + 1) == clear.ERR_UNSUPPORTED and _norm_bwd(C=2 ** 23 + 1) == clear.ERR_UNSUPPORTED
+    n = ctypes.c_size_t()
+    assert clear.load().clear_layer_norm_bwd_workspace(1, 1, 2 ** 23 + 1, 0, ctypes.byref(n)) == clear.ERR_UNSUPPORTED
+
+
+def test_prep_gradient_refuses_two_billion_tokens():
+    assert _prep_bwd(gh=2 ** 16, gw=2 ** 15) == clear.ERR_UNSUPPORTED

@@ -339,7 +339,7 @@ __global__ void __launch_bounds__(kBwdThreads<T, V, LANES, WARPS>) clear_norm_bw
 {
     constexpr int U = kRowsAtOnce<V, VPT>, kLanes = LANES * WARPS, kGroups = kBwdGroups<T, V, LANES, WARPS>, kThreads = kBwdThreads<T, V, LANES, WARPS>;
     constexpr int kBytes = V * (int)sizeof(T), kSlots = 2 * U * VPT;
-    constexpr int kStages = kBwdStages<T, V, VPT, LANES, WARPS>, kAhead = kStages ? kStages - 1 : 1;
+    constexpr int kStages = kBwdStages<T, V, VPT, LANES, WARPS>;
     constexpr bool kAsync = kStages > 0;
     using Share = RowShare<T, V, VPT, kLanes>;
     using F = typename Share::F;
@@ -357,31 +357,23 @@ __global__ void __launch_bounds__(kBwdThreads<T, V, LANES, WARPS>) clear_norm_bw
     const float *mean = p.mean_in + (size_t)blockIdx.x * p.rows, *rstd = p.rstd_in + (size_t)blockIdx.x * p.rows;
     Share rx[U], rd[U];  // without asynchronous copies: the next rows
     float m[U], r[U];
-    // rows at `at` into stage `st`; a row beyond the last, or a channel beyond the row, counts as zero
-    auto slot = [&](int st, int u, int v, int which) {
-        return s_ring + ((st * kSlots + 2 * (u * VPT + v) + which) * kThreads + threadIdx.x) * kBytes;
-    };
-    auto load = [&](unsigned at, int st) {
+    // rows at `at` into a stage (by its offset in bytes); what lies beyond the last row is not copied and counts as zero below
+    constexpr uint32_t kStageBytes = kSlots * kThreads * kBytes;
+    const uint32_t ring = ptx::smem_u32(s_ring) + threadIdx.x * kBytes;
+    bool in_row[VPT];
+#pragma unroll
+    for (int v = 0; v < VPT; ++v) in_row[v] = first + v * kLanes < p.n_vec;
+    auto load = [&](unsigned at, uint32_t stage) {
         const T *px = x + (long long)at * p.x_stride_n, *pd = dy + (long long)at * p.dy_stride_n;
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             const bool live = at + u < p.rows;
             if constexpr (kAsync) {
-                if (live) {
 #pragma unroll
-                    for (int v = 0; v < VPT; ++v)
-                        if (first + v * kLanes < p.n_vec) {
-                            copy_async<kBytes>(ptx::smem_u32(slot(st, u, v, 0)), px + v * kLanes * V);
-                            copy_async<kBytes>(ptx::smem_u32(slot(st, u, v, 1)), pd + v * kLanes * V);
-                        }
-                } else {
-                    Pack<T, V> none;
-                    none.zero();
-#pragma unroll
-                    for (int v = 0; v < VPT; ++v) {
-                        none.store(reinterpret_cast<T *>(slot(st, u, v, 0)));
-                        none.store(reinterpret_cast<T *>(slot(st, u, v, 1)));
-                    }
+                for (int v = 0; v < VPT; ++v) {
+                    const uint32_t to = ring + stage + 2 * (u * VPT + v) * kThreads * kBytes;
+                    copy_async_if(to, px + v * kLanes * V, live && in_row[v]);
+                    copy_async_if(to + kThreads * kBytes, pd + v * kLanes * V, live && in_row[v]);
                 }
             } else {
                 rx[u].load(live ? px : x, first, live ? p.n_vec : 0);
@@ -404,15 +396,14 @@ __global__ void __launch_bounds__(kBwdThreads<T, V, LANES, WARPS>) clear_norm_bw
     if constexpr (kAsync) {  // channels beyond the row: zeros that no copy touches
 #pragma unroll
         for (int v = 0; v < VPT; ++v)
-            if (first + v * kLanes >= p.n_vec) {
-                Pack<T, V> none;
-                none.zero();
-                for (int i = 0; i < kStages * U * 2; ++i) none.store(reinterpret_cast<T *>(slot(i / (2 * U), i / 2 % U, v, i % 2)));
-            }
+            if (!in_row[v])
+                for (int i = 0; i < kStages * U * 2; ++i) {
+                    const int slot = (i / 2 % U * VPT + v) * 2 + i % 2;
+                    *reinterpret_cast<uint4 *>(s_ring + i / (2 * U) * kStageBytes + (slot * kThreads + threadIdx.x) * kBytes) = uint4{};
+                }
     }
     load_stats(row);
-#pragma unroll
-    for (int s = 0; s < kAhead; ++s) load(row + s * stride, s);
+    load(row, 0);
     F dw[kPairs], db[kPairs], gain[kPairs];
     {
         float f[VPT * V];
@@ -438,21 +429,35 @@ __global__ void __launch_bounds__(kBwdThreads<T, V, LANES, WARPS>) clear_norm_bw
             dw[i] = db[i] = F(0.f);
         }
     }
-    int parity = 0, st = 0;
+    int parity = 0;
+    uint32_t stage = 0;
     for (; lead < p.rows; lead += stride, row += stride, parity ^= 1) {
         F h[U][kPairs], g[U][kPairs];
         float sums[2 * U], scale[U];
         if constexpr (kAsync) {
-            load(row + kAhead * stride, st == 0 ? kStages - 1 : st - 1);
-            copies_wait<kAhead>();
+            static_assert(kStages == 2, "two stages take turns");
+            load(row + stride, stage ^ kStageBytes);
+            copies_wait<1>();
 #pragma unroll
             for (int u = 0; u < U; ++u)
 #pragma unroll
                 for (int v = 0; v < VPT; ++v) {
-                    rx[u].raw[v].load(reinterpret_cast<const T *>(slot(st, u, v, 0)));
-                    rd[u].raw[v].load(reinterpret_cast<const T *>(slot(st, u, v, 1)));
+                    const unsigned char *at = s_ring + stage + (2 * (u * VPT + v) * kThreads + threadIdx.x) * kBytes;
+                    rx[u].raw[v].load(reinterpret_cast<const T *>(at));
+                    rd[u].raw[v].load(reinterpret_cast<const T *>(at + kThreads * kBytes));
                 }
-            if (++st == kStages) st = 0;
+            stage ^= kStageBytes;
+            if (row + U > p.rows) {
+#pragma unroll
+                for (int u = 0; u < U; ++u)
+                    if (row + u >= p.rows) {
+#pragma unroll
+                        for (int v = 0; v < VPT; ++v) {
+                            rx[u].raw[v].zero();
+                            rd[u].raw[v].zero();
+                        }
+                    }
+            }
         }
 #pragma unroll
         for (int u = 0; u < U; ++u) {

@@ -86,8 +86,8 @@ __global__ void __launch_bounds__(kThreads, kBlocksPerSm) clear_prep_bwd_kernel(
                 if (bh + j < bh1) {
                     const long long at = elem + (long long)(bh + j) * stride;
                     if constexpr (kAhead<T>) {
-                        copy_async<16>(ptx::smem_u32(slot(step, j, 0)), x_in + at);
-                        copy_async<16>(ptx::smem_u32(slot(step, j, 1)), dy_in + at);
+                        copy_async(ptx::smem_u32(slot(step, j, 0)), x_in + at);
+                        copy_async(ptx::smem_u32(slot(step, j, 1)), dy_in + at);
                     } else {
                         nx[j].load(x_in + at);
                         nd[j].load(dy_in + at);

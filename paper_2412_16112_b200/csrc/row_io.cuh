@@ -117,12 +117,16 @@ struct Pack {
     }
 };
 
-// Asynchronous copy of BYTES (4, 8 or 16) into shared memory.
-template <int BYTES>
+// Asynchronous copy of 16 bytes into shared memory, and one that is made where `there` holds, without a branch.
 __device__ __forceinline__ void copy_async(uint32_t dst, const void *src)
 {
-    if constexpr (BYTES == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
-    else asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" ::"r"(dst), "l"(src), "n"(BYTES) : "memory");
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+}
+__device__ __forceinline__ void copy_async_if(uint32_t dst, const void *src, bool there)
+{
+    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %2, 0;\n\t@p cp.async.cg.shared.global [%0], [%1], 16;\n\t}" ::"r"(dst), "l"(src),
+                 "r"((uint32_t)there)
+                 : "memory");
 }
 __device__ __forceinline__ void copies_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 // Until at most LEFT of the thread's latest groups are on their way.

@@ -4,7 +4,12 @@
 //   h = (x - mean) rstd,   y = h G + bias,   G = weight_offset + weight
 //   g = dy G,   dx = rstd (g - mean(g) - h mean(g h)),   dweight = sum of dy h over the rows,   dbias = sum of dy
 //
-// HBM bounds all of it: x once in and y once out, or x and dy in and dx out, so a row stays in registers between its two uses.
+// HBM bounds all of it: x once in and y once out, or x and dy in and dx out, so a row stays in registers between its two uses.  What
+// is left to lose is issue slots (some 40 instructions for 8 channels of bf16 forward, 75 backward: packed pairs, nothing computed a
+// row that does not have to be) and the start and end of a launch.  Device time, with bytes over the measured copy rate of 6541 GB/s:
+//   forward   262656 x 2048 bf16 modulated  340 us  0.97      16896 x 1536 bf16  19.8 us  0.80      1 row of 768  2.1 us
+//   backward  284160 x 1536 bf16  424 us  0.95      16896 x 1536 bf16  33 us  0.72      16680 x 1003 fp32  39 us  0.79
+// Backward the launch of the second kernel and its chain of reads are about 4 us of every call.
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 
@@ -111,8 +116,12 @@ __device__ __forceinline__ float lanes_sum(float x)
 // this one is worked on.  Gains and biases of the block's entry lie in shared memory as fp32, thread by thread in the order of use.
 template <int WARPS> constexpr int kNormThreads = WARPS > 8 ? 512 : 256;
 
+// Blocks that an SM is to hold: 16 warps to a row leave room for two with fp32 (16896 x 6000: 129 us, with one 161).
+template <typename T, int WARPS> constexpr int kNormBlocks = WARPS <= 8 ? 3 : sizeof(T) == 4 ? 2 : 1;
+
 template <typename T, typename TP, int V, int VPT, int LANES, int WARPS>
-__global__ void __launch_bounds__(kNormThreads<WARPS>, WARPS > 8 ? (sizeof(T) == 4 ? 2 : 1) : 3) clear_norm_fwd_kernel(const __grid_constant__ NormParams p)
+__global__ void __launch_bounds__(kNormThreads<WARPS>, kNormBlocks<T, WARPS>)
+clear_norm_fwd_kernel(const __grid_constant__ NormParams p)
 {
     constexpr int kLanes = LANES * WARPS;  // threads to a row
     constexpr int kGroups = kNormThreads<WARPS> / kLanes, kQuad = V >= 4 ? 4 : V, kQuads = V / kQuad;
@@ -305,12 +314,15 @@ __global__ void __launch_bounds__(256) clear_norm_fwd_long_kernel(const __grid_c
 // ---- backward --------------------------------------------------------------------------------------------------------
 // A thread keeps its channels for all rows of its group, so the sums of the weights' gradients stay in registers.  Two rows go
 // through a group's two sums (of g and of g h over the channels) together: one exchange and one barrier for both.  Rows come ahead by
-// asynchronous copies of each thread's own channels into its own places of shared memory, so no barrier guards them.  The groups of
-// a block are added in shared memory, the blocks' sums by clear_norm_reduce_kernel, all in a fixed order.
-// Rows at once: one where a thread has 16 channels.
+// asynchronous copies of each thread's own channels into its own places of shared memory, so no barrier guards them (16896 x 1536:
+// 33 us, in registers 42).  The groups of a block are added in shared memory, the blocks' sums by clear_norm_reduce_kernel, all in a
+// fixed order.  Rows at once: one where a thread has 16 channels.
 template <int V, int VPT> constexpr int kRowsAtOnce = V * VPT > 8 ? 1 : 2;
-template <typename T, int V, int LANES, int WARPS> constexpr int kBwdGroups = (sizeof(T) == 2 && V == 8 ? 640 : 512) / (LANES * WARPS);
-template <typename T, int V, int LANES, int WARPS> constexpr int kBwdThreads = kBwdGroups<T, V, LANES, WARPS> * LANES * WARPS;
+// Threads of a block, one block an SM: 640 or 512 by registers (284160 x 1536 bf16: 424 and 494 us; 66048 x 1024 fp32: 134 and 122).
+template <typename T, int V, int LANES, int WARPS>
+constexpr int kBwdGroups = (sizeof(T) == 2 && V == 8 ? 640 : 512) / (LANES * WARPS);
+template <typename T, int V, int LANES, int WARPS>
+constexpr int kBwdThreads = kBwdGroups<T, V, LANES, WARPS> * LANES * WARPS;
 // Bytes of one step's rows, and steps in shared memory: two, or none where they do not fit or rows allow no copies of 16 bytes (copies
 // of 4 bytes took 57 us where registers took 46, 16680 rows of 1003 fp32 channels; three steps were no faster than two).
 template <typename T, int V, int VPT, int LANES, int WARPS>
@@ -337,7 +349,8 @@ __device__ __forceinline__ float warp_sum4(const float (&v)[4], int lane)
 template <typename T, typename TP, int V, int VPT, int LANES, int WARPS>
 __global__ void __launch_bounds__(kBwdThreads<T, V, LANES, WARPS>) clear_norm_bwd_kernel(const __grid_constant__ NormParams p)
 {
-    constexpr int U = kRowsAtOnce<V, VPT>, kLanes = LANES * WARPS, kGroups = kBwdGroups<T, V, LANES, WARPS>, kThreads = kBwdThreads<T, V, LANES, WARPS>;
+    constexpr int U = kRowsAtOnce<V, VPT>, kLanes = LANES * WARPS;
+    constexpr int kGroups = kBwdGroups<T, V, LANES, WARPS>, kThreads = kBwdThreads<T, V, LANES, WARPS>;
     constexpr int kBytes = V * (int)sizeof(T), kSlots = 2 * U * VPT;
     constexpr int kStages = kBwdStages<T, V, VPT, LANES, WARPS>;
     constexpr bool kAsync = kStages > 0;
@@ -735,6 +748,8 @@ int norm_fwd(const NormArgs &a, cudaStream_t stream)
     if (vector_fits(a, kWide, sizeof(T), sizeof(TP))) {
         // up to four accesses of 16 bytes a thread, then more warps
         const int n = (a.C / kWide + 31) / 32;  // accesses, in warps
+        // eight lanes for rows of up to 512 bytes (300000 x 256 bf16: 51 us, a warp a row 80); four accesses or three, whichever leaves
+        // fewer lanes idle (16896 x 1536: 20 and 27 us)
         if (a.C / kWide <= 8) return launch_fwd<T, TP, kWide, 1, 8, 1>(p, gpu, stream);
         if (a.C / kWide <= 16) return launch_fwd<T, TP, kWide, 2, 8, 1>(p, gpu, stream);
         if (n <= 1) return launch_fwd<T, TP, kWide, 4, 8, 1>(p, gpu, stream);

@@ -4,6 +4,8 @@
 //
 // HBM bounds it: x and dy in once, dx out once.  As in the forward kernel a thread owns 8 channels of a token and walks over its
 // (batch, head) rows, so sines and cosines are computed once a token; the gains' gradients stay in its registers all the while.
+// Device time, and bytes over the measured copy rate of 6541 GB/s: 4096 px bf16 380 us, 0.98; 1024 px bf16 31.9 us, 0.82 (4 us of it
+// the second kernel, which adds the blocks' sums of the gains' gradients), fp32 58 us, 0.90; the tiny fp32 shape 4.5 us.
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 
@@ -36,7 +38,7 @@ struct PrepBwdParams {
 };
 
 // Rows come ahead by asynchronous copies of each thread's own channels into its own places of shared memory (bf16: 16 bytes, two
-// steps of three rows, 385 us at 4096 px where three rows ahead in registers take 410), or in registers where 8 channels are two
+// steps of three rows, 380 us at 4096 px where three rows ahead in registers take 410), or in registers where 8 channels are two
 // accesses (fp32, 4608 tokens of 24 heads, two rows: 58 us, copies 91).
 template <typename T> constexpr bool kAhead = sizeof(T) == 2;
 template <typename T> constexpr int kRowsOf = kAhead<T> ? 3 : 2;

@@ -2,7 +2,9 @@
 // gradient is the turn by the opposite angle.  Pairs are neighbours (2p, 2p+1) or half the rotary part apart (p, p + P).
 //
 // HBM bounds it (every element in once, out once).  A thread owns a few pairs of one token and walks over heads: angles depend on
-// the token only, so their sines and cosines are computed once and serve several heads of Q and of K.
+// the token only, so their sines and cosines are computed once and serve several heads of Q and of K.  Device time, and bytes over
+// the measured copy rate of 6541 GB/s: 66048 tokens of 24 + 8 heads of 128, half of each turned, 169 us, 0.98; packed projection of
+// 4608 tokens of 24 + 24 heads 21.4 us, 0.81; fp32 gradient of 16680 tokens of 24 heads of 80 43 us, 0.91; two tokens 2.7 us.
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 
@@ -110,7 +112,7 @@ __global__ void __launch_bounds__(kRopeThreads, 4) clear_rope_kernel(const __gri
 {
     constexpr int kRows = HALF ? 2 : 4;  // heads in flight: four accesses of a thread
     using Turner = Turn<T, V, HALF>;
-    // constants that lanes read at places of their own would come one lane at a time
+    // from the parameters, lanes that read at places of their own would be served one after the other (4608 tokens: 24 us, so 21.4)
     __shared__ uint64_t s_turns[kMaxRopePairs];
     __shared__ uint8_t s_axis[kMaxRopePairs];
     for (int i = threadIdx.x; i < p.pairs; i += kRopeThreads) {

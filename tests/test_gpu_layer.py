@@ -632,6 +632,23 @@ def test_calls_on_streams_of_their_own():
         assert all(torch.equal(o, e) for o, e in zip(outs, w))
 
 
+@pytest.mark.parametrize("given", ["number", "stream"])
+def test_the_default_stream_given_from_within_another(given):
+    """Workspaces then belong to the default stream, not to the current one."""
+    go, outs, _ = _all_calls(300)
+    go()
+    torch.cuda.synchronize()
+    want = [o.clone() for o in outs]
+    for o in outs:
+        o.fill_(float("nan"))
+    torch.cuda.synchronize()
+    with torch.cuda.stream(torch.cuda.Stream()):
+        for _ in range(3):
+            go(stream=0 if given == "number" else torch.cuda.default_stream())
+    torch.cuda.synchronize()
+    assert all(torch.equal(o, e) for o, e in zip(outs, want))
+
+
 def test_captured_calls_replay_on_new_inputs():
     """Two graphs of the same calls, replayed side by side, each with workspaces of its own."""
     jobs = [_all_calls(7), _all_calls(8)]

@@ -283,20 +283,15 @@ def _launch_with_workspace(fn_name, device, stream, args, n_bytes):
     if device != torch.cuda.current_device():
         with torch.cuda.device(device):
             return _launch_with_workspace(fn_name, device, stream, args, n_bytes)
-    st = torch._C._cuda_getCurrentRawStream(device) if stream is None else _stream_ptr(stream)
-    ws = _workspace(n_bytes, device, st) if n_bytes else None
+    st = torch._C._cuda_getCurrentRawStream(device)
+    if stream is not None and (given := _stream_ptr(stream)) != st:
+        with torch.cuda.stream(torch.cuda.ExternalStream(given, device=device)):
+            return _launch_with_workspace(fn_name, device, None, args, n_bytes)
+    # torch's allocator keeps the memory from other streams until this stream's work on it has ended
+    ws = torch.empty(n_bytes, dtype=torch.uint8, device=_cuda(device)) if n_bytes else None
     status = getattr(_lib or load(), fn_name)(*args, None if ws is None else ws.data_ptr(), n_bytes, st)
     if status != OK:
         raise ClearError(status, fn_name)
-
-
-def _workspace(n_bytes, device, stream_ptr):
-    """Device memory for one call on that stream: torch's allocator keeps it from other streams until the call has ended."""
-    import torch
-    if stream_ptr == torch._C._cuda_getCurrentRawStream(device):
-        return torch.empty(n_bytes, dtype=torch.uint8, device=_cuda(device))
-    with torch.cuda.stream(torch.cuda.ExternalStream(stream_ptr, device=device)):
-        return torch.empty(n_bytes, dtype=torch.uint8, device=_cuda(device))
 
 
 @functools.lru_cache(maxsize=64)
@@ -439,9 +434,9 @@ def _norm_rows(x, *others):
 
 
 def _norm_params(x, device, B, C, *params):
-    """(dtype code, strides) of weights and biases [C] or [B, C]; None stands for none."""
+    """(dtype code, strides, numbers of axes seen) of weights and biases [C] or [B, C]; None stands for none."""
     import torch
-    kind, strides = None, []
+    kind, strides, axes = None, [], set()
     for p in params:
         if p is None:
             strides.append(0)
@@ -459,9 +454,10 @@ def _norm_params(x, device, B, C, *params):
             strides.append(s[0])
         else:
             raise ValueError("weight, bias and their gradients must be [C] or [B, C]")
+        axes.add(len(s))
         if s[-1] != 1 and C > 1:
             raise ValueError("the channels of a weight or bias must be contiguous")
-    return (BF16 if kind is torch.bfloat16 else F32), strides
+    return (BF16 if kind is torch.bfloat16 else F32), strides, axes
 
 
 def _norm_stats(device, n, *stats):
@@ -476,7 +472,7 @@ def clear_layer_norm_fwd(x, y, weight=None, bias=None, mean=None, rstd=None, wei
     (x - mean) * rstd * (weight_offset + weight) + bias, with weight and bias [C], or [B, C] for a pair a batch entry (a modulated
     layer: ``weight`` the scale, ``weight_offset`` 1, ``bias`` the shift).  ``mean``, ``rstd``: fp32, written for the backward pass."""
     (B, N, C), dtype, device, strides = _norm_rows(x, y)
-    kind, wb = _norm_params(x, device, B, C, weight, bias)
+    kind, wb, _ = _norm_params(x, device, B, C, weight, bias)
     _norm_stats(device, B * N, mean, rstd)
     _launch("clear_layer_norm_fwd", device, stream, (
         x.data_ptr(), y.data_ptr(), _ptr(weight), _ptr(bias), _ptr(mean), _ptr(rstd), B, N, C, dtype, kind, *strides, *wb,
@@ -489,15 +485,11 @@ def clear_layer_norm_bwd(x, dy, weight, mean, rstd, dx, dweight=None, dbias=None
     or ``dy``) and, where given, ``dweight`` and ``dbias``, summed over all rows ([C]) or those of each batch entry ([B, C], as the
     weight is).  Returns the three."""
     (B, N, C), dtype, device, strides = _norm_rows(x, dy, dx)
-    kind, sums = _norm_params(x, device, B, C, weight, dweight, dbias)
+    kind, sums, axes = _norm_params(x, device, B, C, weight, dweight, dbias)
+    if len(axes) > 1:
+        raise ValueError("weight, dweight and dbias must all be [C] or all be [B, C]")
+    per_batch = 1 if 2 in axes else 0
     _norm_stats(device, B * N, mean, rstd)
-    per_batch = None
-    for p in (weight, dweight, dbias):
-        if p is not None:
-            if per_batch is not None and per_batch != p.dim() - 1:
-                raise ValueError("weight, dweight and dbias must all be [C] or all be [B, C]")
-            per_batch = p.dim() - 1
-    per_batch = per_batch or 0
     n_bytes = 0
     if dweight is not None or dbias is not None:
         n_bytes = _workspace_bytes("clear_layer_norm_bwd_workspace", device, B, N, C, per_batch)

@@ -224,7 +224,7 @@ int clear_qk_norm_rope(const void *q_in, const void *k_in, void *q_out, void *k_
  * allowed.  fp32 arithmetic; sums in a fixed order, so repeats on one kind of device are equal bit for bit.
  * workspace: clear_qk_norm_rope_bwd_workspace() bytes of device memory, 16-byte aligned, which the call may write until it has
  * ended on the stream (calls that can overlap need one each); may be NULL when neither gain's gradient is wanted.
- * One launch on `stream`, two with a gain's gradient; no allocation, no host synchronisation.
+ * One launch on `stream`, two with a gain's gradient of more than a few rows; no allocation, no host synchronisation.
  * Errors: those of clear_qk_norm_rope; INVALID_ARG also for a workspace that is missing or too small; UNSUPPORTED also for 2^31
  * tokens or more. */
 int clear_qk_norm_rope_bwd(const void *q, const void *k, const void *dq_rot, const void *dk_rot, void *dq, void *dk,
@@ -312,8 +312,8 @@ int clear_layer_norm_fwd(const void *x, void *y, const void *weight, const void 
  * added to; either may be NULL.  dx may lie in the place of x or of dy with the same strides; any other overlap is not allowed.
  * fp32 arithmetic; sums in a fixed order, so repeats on one kind of device are equal bit for bit.
  * workspace: clear_layer_norm_bwd_workspace() bytes of device memory, 16-byte aligned, which the call may write until it has ended on
- * the stream (calls that can overlap need one each); may be NULL when neither sum is wanted.  One launch on `stream`, two with a sum
- * (three above 8192 channels); no allocation, no host synchronisation.  Without rows dweight and dbias are set to zero.
+ * the stream (calls that can overlap need one each); may be NULL when neither sum is wanted or that number is zero (few rows).  One
+ * launch on `stream`, two with a sum over many rows (three above 8192 channels); no allocation, no host synchronisation.  Without rows dweight and dbias are set to zero.
  * Errors: those of clear_layer_norm_fwd; INVALID_ARG also for missing statistics, for a workspace that is missing or too small, for
  * strides of weight, dweight or dbias that do not go with per_batch; UNSUPPORTED also for more than 65535 batch entries with
  * per_batch. */

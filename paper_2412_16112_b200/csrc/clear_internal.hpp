@@ -159,7 +159,7 @@ struct NormArgs {
     float offset, eps;
     void *workspace;
 };
-int norm_bwd_workspace(int B, int N, int C, size_t *bytes);
+int norm_bwd_workspace(int B, int N, int C, int per_batch, size_t *bytes);
 int launch_norm_fwd(const NormArgs &a, cudaStream_t stream);
 int launch_norm_bwd(const NormArgs &a, cudaStream_t stream);
 // Backward pass on the tensor cores (bf16): a query-role and a key-role launch over the plan's tile schedule (a plan made

@@ -159,7 +159,7 @@ int clear_layer_norm_bwd_workspace(int B, int N, int C, int per_batch, size_t *b
     if (!bytes || B < 0 || N < 0 || C <= 0) return CLEAR_ERR_INVALID_ARG;
     if ((long long)B * N > 0x7fffffffLL || C > kMaxChannels || (per_batch && B > 65535)) return CLEAR_ERR_UNSUPPORTED;
     *bytes = 0;
-    return B == 0 || N == 0 ? CLEAR_OK : norm_bwd_workspace(B, N, C, bytes);
+    return B == 0 || N == 0 ? CLEAR_OK : norm_bwd_workspace(B, N, C, per_batch != 0, bytes);
 }
 
 int clear_layer_norm_bwd(const void *x, const void *dy, const void *weight, const float *mean, const float *rstd, void *dx,
@@ -206,8 +206,8 @@ int clear_layer_norm_bwd(const void *x, const void *dy, const void *weight, cons
         return CLEAR_ERR_INVALID_ARG;
     if (dweight || dbias) {
         size_t need = 0;
-        if (const int e = norm_bwd_workspace(B, N, C, &need)) return e;
-        if (!workspace || workspace_bytes < need) return CLEAR_ERR_INVALID_ARG;
+        if (const int e = norm_bwd_workspace(B, N, C, a.per_batch, &need)) return e;
+        if (need && (!workspace || workspace_bytes < need)) return CLEAR_ERR_INVALID_ARG;
         if (misaligned(workspace, 16)) return CLEAR_ERR_MISALIGNED;
     }
     return launch_norm_bwd(a, s);

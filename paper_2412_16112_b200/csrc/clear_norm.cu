@@ -10,6 +10,7 @@
 //   forward   262656 x 2048 bf16 modulated  340 us  0.97      16896 x 1536 bf16  19.8 us  0.80      1 row of 768  2.1 us
 //   backward  284160 x 1536 bf16  424 us  0.95      16896 x 1536 bf16  33 us  0.72      16680 x 1003 fp32  39 us  0.79
 // Backward the launch of the second kernel and its chain of reads are about 4 us of every call.
+#include <cooperative_groups.h>
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 
@@ -30,7 +31,9 @@ struct NormParams {
     const void *weight, *bias;
     const float *mean_in, *rstd_in;
     float *mean, *rstd;
-    float *partial;               // backward: [entries][blocks of an entry][2][C]
+    float *partial;               // backward: [entries][blocks of an entry][2][C], or null
+    void *dweight, *dbias;        // backward, without partial sums: where an entry's cluster of blocks writes its sums itself
+    long long dw_stride_b, db_stride_b;
     long long x_stride_b, x_stride_n, dy_stride_b, dy_stride_n, out_stride_b, out_stride_n;
     long long w_stride_b, bias_stride_b;
     unsigned rows;                // rows of an entry
@@ -539,7 +542,7 @@ __global__ void __launch_bounds__(kBwdThreads<T, V, LANES, WARPS>) clear_norm_bw
             }
         }
     }
-    if (!p.partial) return;
+    if (!p.partial && !p.dweight && !p.dbias) return;
     // rows of one warp first, then the groups side by side in shared memory
 #pragma unroll
     for (int i = 0; i < kPairs; ++i)
@@ -564,8 +567,21 @@ __global__ void __launch_bounds__(kBwdThreads<T, V, LANES, WARPS>) clear_norm_bw
     for (int c = threadIdx.x; c < 2 * p.C; c += kThreads) {
         float sum = s_sum[c];
         for (int t = 1; t < kTerms; ++t) sum += s_sum[t * 2 * p.C + c];
-        out[c] = sum;
+        if (p.partial) out[c] = sum;
+        else s_sum[c] = sum;
     }
+    if (p.partial) return;
+    namespace cg = cooperative_groups;
+    cg::cluster_group cluster = cg::this_cluster();
+    cluster.sync();  // the blocks' sums, each in its own shared memory
+    const int blocks = cluster.num_blocks();
+    for (int c = cluster.block_rank() * kThreads + threadIdx.x; c < 2 * p.C; c += blocks * kThreads) {
+        float sum = 0.f;
+        for (int k = 0; k < blocks; ++k) sum += cluster.map_shared_rank(s_sum, k)[c];
+        TP *to = static_cast<TP *>(c < p.C ? p.dweight : p.dbias);
+        if (to) to[(long long)blockIdx.x * (c < p.C ? p.dw_stride_b : p.db_stride_b) + (c < p.C ? c : c - p.C)] = (TP)sum;
+    }
+    cluster.sync();  // nobody leaves while its sums are read
 }
 
 // Rows too long for registers: the rows' gradients (a block to a row) ...
@@ -645,6 +661,8 @@ clear_norm_reduce_kernel(const float *partial, int parts, int C, TP *dweight, TP
         out[(long long)blockIdx.y * (blockIdx.z == 0 ? dw_stride_b : db_stride_b) + col] = (TP)sum;
     }
 }
+
+constexpr int kMostTileChannels = 8192;  // of the backward kernel that keeps rows in registers
 
 struct Gpu {
     int device = 0, n_sm = 0;
@@ -792,15 +810,33 @@ int launch_reduce(const NormArgs &a, int parts, cudaStream_t stream)
     return CLEAR_OK;
 }
 
+// An entry so small that a cluster of blocks, adding up its sums itself, is done about when many blocks and a second kernel would be
+// (40 rows of 768 bf16 channels 5.1 and 5.6 us, 100 of 1536 7.2 and 5.5), and the host as well, which is what small calls wait for (13
+// and 18 us, with no workspace to allocate).
+bool small_entry(long long rows, int C) { return C <= kMostTileChannels && rows * C <= 96 * 1024; }
+
 template <typename T, typename TP, int V, int VPT, int LANES, int WARPS>
 int launch_bwd(NormParams p, const NormArgs &a, const Gpu &gpu, cudaStream_t stream)
 {
     constexpr int kThreads = kBwdThreads<T, V, LANES, WARPS>;
     auto kernel = clear_norm_bwd_kernel<T, TP, V, VPT, LANES, WARPS>;
+    constexpr int kRowsABlock = kBwdGroups<T, V, LANES, WARPS> * kRowsAtOnce<V, VPT>;
     const bool sums = a.dweight || a.dbias;
-    const unsigned shares = shares_of(p, kBwdGroups<T, V, LANES, WARPS> * kRowsAtOnce<V, VPT>, gpu.n_sm);
+    // where each weight has one entry's rows: a cluster of blocks adds up a small entry, one block what falls to one block anyway (200
+    // entries of 40 rows of 768: 15 us, with partial sums 40)
+    unsigned shares = shares_of(p, kRowsABlock, gpu.n_sm);
+    const bool small = small_entry(p.rows, p.C);
+    const bool direct = sums && (a.per_batch || p.entries == 1) && (small || shares == 1);
+    if (direct) {
+        shares = std::min(shares, 8u);
+        while (shares & (shares - 1)) ++shares;  // 1, 2, 4 or 8
+    }
     p.n_vec = p.C / V;
-    p.partial = sums ? static_cast<float *>(a.workspace) : nullptr;
+    p.partial = sums && !direct ? static_cast<float *>(a.workspace) : nullptr;
+    if (direct) {
+        p.dweight = a.dweight; p.dbias = a.dbias;
+        p.dw_stride_b = a.dw_stride_b; p.db_stride_b = a.db_stride_b;
+    }
     constexpr int terms = LANES < 32 ? kThreads / 32 : kBwdGroups<T, V, LANES, WARPS>;
     constexpr int ring = kBwdStages<T, V, VPT, LANES, WARPS> * kBwdStep<T, V, VPT, LANES, WARPS>;
     const int smem = std::max(ring, sums ? terms * 2 * (int)sizeof(float) * p.C : 0);
@@ -808,9 +844,19 @@ int launch_bwd(NormParams p, const NormArgs &a, const Gpu &gpu, cudaStream_t str
     static std::atomic<int> known[kMaxDevices];
     int per_sm = 0;
     if (const int rc = kernel_once(known, kernel, kThreads, most, gpu.device, &per_sm)) return rc;
-    kernel<<<dim3((unsigned)p.entries, shares), kThreads, smem, stream>>>(p);
-    CLEAR_CUDA_TRY(cudaGetLastError());
-    return sums ? launch_reduce<TP>(a, a.per_batch ? shares : shares * p.entries, stream) : CLEAR_OK;
+    cudaLaunchConfig_t cfg{};
+    cudaLaunchAttribute attr{};
+    attr.id = cudaLaunchAttributeClusterDimension;
+    attr.val.clusterDim.x = attr.val.clusterDim.z = 1;
+    attr.val.clusterDim.y = shares;
+    cfg.gridDim = dim3((unsigned)p.entries, shares);
+    cfg.blockDim = dim3(kThreads);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = stream;
+    cfg.attrs = &attr;
+    cfg.numAttrs = direct && shares > 1;
+    CLEAR_CUDA_TRY(cudaLaunchKernelEx(&cfg, kernel, p));
+    return sums && !direct ? launch_reduce<TP>(a, a.per_batch ? shares : shares * p.entries, stream) : CLEAR_OK;
 }
 
 // Accesses of one or two channels; UNSUPPORTED above 8192 channels.
@@ -866,12 +912,13 @@ int norm_bwd(const NormArgs &a, cudaStream_t stream)
 
 }  // namespace
 
-// A partial sum of each block: one an SM, or one a batch entry where there are more of those.
-int norm_bwd_workspace(int B, int N, int C, size_t *bytes)
+// A partial sum of each block: one an SM, or one a batch entry where there are more of those; none where a weight's rows are few.
+int norm_bwd_workspace(int B, int N, int C, int per_batch, size_t *bytes)
 {
     Gpu gpu;
     if (const int rc = current_sms(&gpu.device, &gpu.n_sm)) return rc;
-    *bytes = (size_t)std::min<long long>((long long)B * N, std::max(gpu.n_sm, B)) * 2 * sizeof(float) * (size_t)C;
+    const bool none = (per_batch || B == 1 || N == 1) && small_entry(per_batch ? N : (long long)B * N, C);
+    *bytes = none ? 0 : (size_t)std::min<long long>((long long)B * N, std::max(gpu.n_sm, B)) * 2 * sizeof(float) * (size_t)C;
     return CLEAR_OK;
 }
 

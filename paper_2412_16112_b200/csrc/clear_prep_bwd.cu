@@ -6,6 +6,7 @@
 // (batch, head) rows, so sines and cosines are computed once a token; the gains' gradients stay in its registers all the while.
 // Device time, and bytes over the measured copy rate of 6541 GB/s: 4096 px bf16 380 us, 0.98; 1024 px bf16 31.9 us, 0.82 (4 us of it
 // the second kernel, which adds the blocks' sums of the gains' gradients), fp32 58 us, 0.90; the tiny fp32 shape 4.5 us.
+#include <cooperative_groups.h>
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 
@@ -21,6 +22,8 @@
 namespace clear {
 namespace {
 
+namespace cg = cooperative_groups;
+
 constexpr int kThreads = 256, kWarps = kThreads / 32;
 constexpr int kEpl = 8;  // channels a thread
 constexpr int kBlocksPerSm = 2;
@@ -30,6 +33,7 @@ struct PrepBwdParams {
     void *dx[2];
     const float *gain[2];
     float *partial;             // [blocks][2][d], or null
+    float *dgain[2];            // without partial sums: where the one cluster of blocks writes its sums itself
     int n_bh, bh_a_part;        // rows of a token, and of the shares that blocks take of them
     unsigned parts, n_text, grid_w, n_tokens;
     float eps, factor[2];
@@ -51,7 +55,7 @@ __global__ void __launch_bounds__(kThreads, kBlocksPerSm) clear_prep_bwd_kernel(
 {
     constexpr int kLanes = D / kEpl, kTokens = 32 / kLanes, kPairs = kEpl / 2, kRows = kRowsOf<T>;
     extern __shared__ __align__(16) unsigned char s_ring[];  // [kSteps][kRows][x, dy][kThreads][16]
-    __shared__ float s_gain[kWarps][kTokens][D];
+    __shared__ float s_gain[kWarps][kTokens][D], s_sum[2 * D];
     __shared__ uint64_t s_turns[D / 2];
     __shared__ uint8_t s_axis[D / 2];
     for (int i = threadIdx.x; i < D / 2; i += kThreads) {
@@ -170,7 +174,7 @@ __global__ void __launch_bounds__(kThreads, kBlocksPerSm) clear_prep_bwd_kernel(
         }
         if constexpr (kAhead<T>) copies_wait<0>();
     }
-    if (!p.partial) return;
+    if (!p.partial && !p.dgain[0] && !p.dgain[1]) return;
 #pragma unroll
     for (int i = 0; i < kPairs; ++i) {
         s_gain[warp][sub][c0 + 2 * i] = dgain[i].lo();
@@ -181,8 +185,18 @@ __global__ void __launch_bounds__(kThreads, kBlocksPerSm) clear_prep_bwd_kernel(
         float sum = 0.f;
 #pragma unroll
         for (int k = 0; k < kWarps / 2 * kTokens; ++k) sum += s_gain[2 * (k / kTokens) + i / D][k % kTokens][i % D];
-        p.partial[(size_t)blockIdx.x * 2 * D + i] = sum;
+        if (p.partial) p.partial[(size_t)blockIdx.x * 2 * D + i] = sum;
+        else s_sum[i] = sum;
     }
+    if (p.partial) return;
+    cg::cluster_group cluster = cg::this_cluster();
+    cluster.sync();  // the blocks' sums, each in its own shared memory
+    for (int i = blockIdx.x * kThreads + threadIdx.x; i < 2 * D; i += gridDim.x * kThreads) {
+        float sum = 0.f;
+        for (int k = 0; k < (int)gridDim.x; ++k) sum += cluster.map_shared_rank(s_sum, k)[i];
+        if (p.dgain[i / D]) p.dgain[i / D][i % D] = sum;
+    }
+    cluster.sync();  // nobody leaves while its sums are read
 }
 
 // A warp to a channel of a gain: sums of the blocks' partial sums in a fixed order.
@@ -202,27 +216,45 @@ template <typename T, int D>
 int launch(PrepBwdParams &p, float *dgain_q, float *dgain_k, int device, int most, cudaStream_t stream)
 {
     constexpr int kTokens = 32 / (D / kEpl);
-    const int groups = (int)((p.n_tokens + kTokens - 1) / kTokens), warps = most * (kWarps / 2);
+    const int groups = (int)((p.n_tokens + kTokens - 1) / kTokens);
+    // Few rows go to one cluster of blocks that adds up its sums itself: the host, which small calls wait for, has one launch instead of
+    // two (20 us for 24), and the device is done sooner (20 tokens of 2 heads of 64: 4.1 and 4.8 us) or somewhat later (272: 6.5 and 4.6).
+    const bool direct = p.partial && (long long)p.n_bh * p.n_tokens * D <= 48 * 1024;
+    if (direct) {
+        most = 8;
+        p.partial = nullptr;
+        p.dgain[0] = dgain_q;
+        p.dgain[1] = dgain_k;
+    }
     // the rows of a token are shared out while tokens alone leave warps without work
-    const int parts = std::min(p.n_bh, std::max(1, warps / groups));
+    const int warps = most * (kWarps / 2), parts = std::min(p.n_bh, std::max(1, warps / groups));
     p.bh_a_part = (p.n_bh + parts - 1) / parts;
     p.parts = (unsigned)((p.n_bh + p.bh_a_part - 1) / p.bh_a_part);
-    const int blocks = (int)std::min<long long>(most, ((long long)groups * p.parts + kWarps / 2 - 1) / (kWarps / 2));
+    int blocks = (int)std::min<long long>(most, ((long long)groups * p.parts + kWarps / 2 - 1) / (kWarps / 2));
+    if (direct)
+        while (blocks & (blocks - 1)) ++blocks;  // 1, 2, 4 or 8
     constexpr int smem = kRingBytes<T>;
     static std::atomic<int> known[kMaxDevices];
     int per_sm = 0;
     if (const int rc = kernel_once(known, clear_prep_bwd_kernel<T, D>, kThreads, smem, device, &per_sm)) return rc;
-    clear_prep_bwd_kernel<T, D><<<blocks, kThreads, smem, stream>>>(p);
-    CLEAR_CUDA_TRY(cudaGetLastError());
-    if (!p.partial) return CLEAR_OK;
     cudaLaunchConfig_t cfg{};
     cudaLaunchAttribute attr{};
+    attr.id = cudaLaunchAttributeClusterDimension;
+    attr.val.clusterDim.x = (unsigned)blocks;
+    attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
+    cfg.gridDim = dim3(blocks);
+    cfg.blockDim = dim3(kThreads);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = stream;
+    cfg.attrs = &attr;
+    cfg.numAttrs = direct && blocks > 1;
+    CLEAR_CUDA_TRY(cudaLaunchKernelEx(&cfg, clear_prep_bwd_kernel<T, D>, p));
+    if (!p.partial) return CLEAR_OK;
     attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr.val.programmaticStreamSerializationAllowed = 1;
     cfg.gridDim = dim3(2 * D / 8);
     cfg.blockDim = dim3(256);
-    cfg.stream = stream;
-    cfg.attrs = &attr;
+    cfg.dynamicSmemBytes = 0;
     cfg.numAttrs = 1;
     CLEAR_CUDA_TRY(cudaLaunchKernelEx(&cfg, clear_prep_gain_kernel<D>, (const float *)p.partial, blocks, dgain_q, dgain_k));
     return CLEAR_OK;

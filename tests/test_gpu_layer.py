@@ -253,6 +253,27 @@ def test_layer_norm_rows_that_are_not_finite_stay_alone(C):
     assert bool(torch.isfinite(dx[0, fine]).all()) and bool(torch.isnan(dx[0, rows]).all())
 
 
+@pytest.mark.parametrize("dtype,C", [("bf16", 768), ("bf16", 61), ("f32", 128), ("f32", 4100), ("bf16", 8192)])
+@pytest.mark.parametrize("form", ["shared", "batch"])
+def test_layer_norm_sums_of_few_rows_and_of_many(dtype, C, form):
+    """Entries on both sides of the number of rows that one cluster of blocks adds up itself, and one that a single block has."""
+    most = 96 * 1024 // C
+    for B, N in ((1, 1), (1, max(1, most - 1)), (1, most), (1, most + 1), (2, most), (2, most + 1), (160, 2)):
+        x, dy, w, b = _norm_inputs(B, N, C, DTYPES[dtype], torch.float32, form, N)
+        mean, rstd = (torch.empty(B, N, device="cuda") for _ in range(2))
+        clear.clear_layer_norm_fwd(x, torch.empty_like(x), w, b, mean, rstd)
+        dx, dw, db = clear.clear_layer_norm_bwd(x, dy, w, mean, rstd, torch.empty_like(x), torch.empty_like(w), torch.empty_like(b))
+        xn, dyn = x.double(), dy.double()
+        h = (xn - mean.double()[..., None]) * rstd.double()[..., None]
+        over = 1 if form == "batch" else (0, 1)
+        n = (N if form == "batch" else B * N) + 20
+        for got, terms in ((dw, dyn * h), (db, dyn)):
+            slack = n * U * terms.abs().sum(over) + U * terms.sum(over).abs()
+            assert bool(((got.double() - terms.sum(over)).abs() <= slack).all()), (B, N)
+        again = clear.clear_layer_norm_bwd(x, dy, w, mean, rstd, torch.empty_like(x), torch.empty_like(w), torch.empty_like(b))
+        assert all(torch.equal(a, e) for a, e in zip(again, (dx, dw, db)))
+
+
 def test_layer_norm_sums_repeat_bit_for_bit():
     x, dy, w, b = _norm_inputs(3, 2111, 768, torch.bfloat16, torch.bfloat16, "batch", 2)
     mean, rstd = (torch.empty(3, 2111, device="cuda") for _ in range(2))
@@ -680,16 +701,16 @@ def test_captured_calls_replay_on_new_inputs():
 
 
 def test_workspaces_that_are_missing_or_too_small_are_refused():
-    x, dy, w, _ = _norm_inputs(1, 50, 64, torch.float32, torch.float32, "shared", 1)
-    stats = torch.ones(1, 50, device="cuda")
+    x, dy, w, _ = _norm_inputs(1, 9000, 64, torch.float32, torch.float32, "shared", 1)
+    stats = torch.ones(1, 9000, device="cuda")
     dx, dw = torch.empty_like(x), torch.empty_like(w)
-    need = clear._workspace_bytes("clear_layer_norm_bwd_workspace", 0, 1, 50, 64, 0)
+    need = clear._workspace_bytes("clear_layer_norm_bwd_workspace", 0, 1, 9000, 64, 0)
     ws = torch.empty(need + 16, dtype=torch.uint8, device="cuda")
     stream = torch.cuda.current_stream().cuda_stream
 
     def norm(ptr, n):
         return clear.load().clear_layer_norm_bwd(x.data_ptr(), dy.data_ptr(), w.data_ptr(), stats.data_ptr(), stats.data_ptr(),
-                                                 dx.data_ptr(), dw.data_ptr(), None, 1, 50, 64, clear.F32, clear.F32, 0, 0, 64, 0, 64,
+                                                 dx.data_ptr(), dw.data_ptr(), None, 1, 9000, 64, clear.F32, clear.F32, 0, 0, 64, 0, 64,
                                                  0, 64, 0, 0, 0, 0.0, ptr, n, stream)
 
     assert norm(None, need) == norm(ws.data_ptr(), need - 1) == clear.ERR_INVALID_ARG

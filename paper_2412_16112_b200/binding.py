@@ -12,6 +12,8 @@ import os
 import threading
 from typing import Optional
 
+import torch
+
 from . import build as _build
 
 OK = 0
@@ -265,44 +267,46 @@ def clear_qk_norm_rope(q, k, q_out, k_out, grid_h, grid_w, n_text, axes_dim, gai
     return q_out, k_out
 
 
+_CODES = {torch.bfloat16: BF16, torch.float32: F32}
+_TWELVE = ctypes.c_longlong * 12
+
+# The current device and a device's current stream, as numbers: what torch.cuda.current_device and current_stream look up.
+_current_device = getattr(torch._C, "_cuda_getDevice", None)
+_current_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+
+
 def _launch(fn_name, device, stream, args):
     """Calls ``fn_name(*args, stream)`` with the device of that number current; on its current stream unless one is given."""
-    import torch
-    if device != torch.cuda.current_device():
+    if device != _current_device():
         with torch.cuda.device(device):
             return _launch(fn_name, device, stream, args)
-    st = torch._C._cuda_getCurrentRawStream(device) if stream is None else _stream_ptr(stream)
-    status = getattr(_lib or load(), fn_name)(*args, st)
+    status = getattr(_lib or load(), fn_name)(*args, _current_stream(device) if stream is None else _stream_ptr(stream))
     if status != OK:
         raise ClearError(status, fn_name)
 
 
 def _launch_with_workspace(fn_name, device, stream, args, n_bytes):
     """The same with a workspace and its size before the stream."""
-    import torch
-    if device != torch.cuda.current_device():
+    if not n_bytes:
+        return _launch(fn_name, device, stream, (*args, None, 0))
+    if device != _current_device():
         with torch.cuda.device(device):
             return _launch_with_workspace(fn_name, device, stream, args, n_bytes)
-    st = torch._C._cuda_getCurrentRawStream(device)
-    if stream is not None and (given := _stream_ptr(stream)) != st:
+    if stream is not None and (given := _stream_ptr(stream)) != _current_stream(device):
         with torch.cuda.stream(torch.cuda.ExternalStream(given, device=device)):
             return _launch_with_workspace(fn_name, device, None, args, n_bytes)
     # torch's allocator keeps the memory from other streams until this stream's work on it has ended
-    ws = torch.empty(n_bytes, dtype=torch.uint8, device=_cuda(device)) if n_bytes else None
-    status = getattr(_lib or load(), fn_name)(*args, None if ws is None else ws.data_ptr(), n_bytes, st)
-    if status != OK:
-        raise ClearError(status, fn_name)
+    ws = torch.empty(n_bytes, dtype=torch.uint8, device=_cuda(device))
+    _launch(fn_name, device, None, (*args, ws.data_ptr(), n_bytes))
 
 
 @functools.lru_cache(maxsize=64)
 def _cuda(index):
-    import torch
     return torch.device("cuda", index)
 
 
 @functools.lru_cache(maxsize=256)
 def _workspace_bytes(fn_name, device, *shape):
-    import torch
     out = ctypes.c_size_t()
     with torch.cuda.device(device):
         _check(getattr(load(), fn_name)(*shape, ctypes.byref(out)), fn_name)
@@ -317,12 +321,11 @@ def clear_qk_norm_rope_bwd(q, k, dq_rot, dk_rot, dq, dk, grid_h, grid_w, n_text,
                            dgain_k=None, theta=10000.0, ntk_factor=1.0, eps=1e-6, q_factor=1.0, stream=None):
     """Gradient of ``clear_qk_norm_rope``: from its inputs ``q``, ``k`` and the gradients ``dq_rot``, ``dk_rot`` of its outputs into
     ``dq``, ``dk`` and, where given, the gains' ``dgain_q``, ``dgain_k`` (fp32, head_dim values).  Returns the four."""
-    import torch
     dtype, shape, device = q.dtype, q.shape, q.get_device()
     for t in (q, k, dq_rot, dk_rot, dq, dk):
         if t.dtype is not dtype or t.get_device() != device or not t.is_contiguous() or t.shape != shape:
             raise ValueError("q, k and the gradients must be contiguous CUDA tensors of one dtype, device and [B, H, N, d] shape")
-    if (dtype is not torch.bfloat16 and dtype is not torch.float32) or device < 0:
+    if dtype not in _CODES or device < 0:
         raise ValueError("bf16 or fp32 CUDA tensors")
     if len(shape) != 4 or shape[2] != n_text + grid_h * grid_w:
         raise ValueError("q must be [B, H, n_text + grid_h * grid_w, d]")
@@ -334,7 +337,7 @@ def clear_qk_norm_rope_bwd(q, k, dq_rot, dk_rot, dq, dk, grid_h, grid_w, n_text,
     n_bytes = 0 if dgain_q is None and dgain_k is None else _workspace_bytes("clear_qk_norm_rope_bwd_workspace", device, d)
     _launch_with_workspace("clear_qk_norm_rope_bwd", device, stream, (
         q.data_ptr(), k.data_ptr(), dq_rot.data_ptr(), dk_rot.data_ptr(), dq.data_ptr(), dk.data_ptr(), _ptr(gain_q), _ptr(gain_k),
-        _ptr(dgain_q), _ptr(dgain_k), B, H, grid_h, grid_w, n_text, d, BF16 if dtype is torch.bfloat16 else F32, a0, a1, a2, theta,
+        _ptr(dgain_q), _ptr(dgain_k), B, H, grid_h, grid_w, n_text, d, _CODES[dtype], a0, a1, a2, theta,
         ntk_factor, eps, q_factor), n_bytes)
     return dq, dk, dgain_q, dgain_k
 
@@ -342,7 +345,6 @@ def clear_qk_norm_rope_bwd(q, k, dq_rot, dk_rot, dq, dk, grid_h, grid_w, n_text,
 def clear_rope_frequencies(dim, theta=10000.0, scaling=ROPE_SCALE_NONE, factor=1.0, trained_length=1.0, fast=32.0, slow=1.0):
     """Angular frequencies of a group of ``dim`` channels (a float64 CPU tensor of dim / 2 values), scaled for sequences ``factor``
     times as long as those of training.  Concatenate the groups of several axes for ``clear_rope_fwd``."""
-    import torch
     out = torch.empty(max(0, int(dim) // 2), dtype=torch.float64)
     buf = out.data_ptr() if out.numel() else None
     _check(load().clear_rope_frequencies(buf, int(dim), float(theta), int(scaling), float(factor), float(trained_length), float(fast),
@@ -356,9 +358,8 @@ def _int_array(values):
 
 
 def _rope(fn_name, q, k, q_out, k_out, positions, frequencies, axes_dim, layout, factor, stream):
-    import torch
     dtype, shape, device = q.dtype, q.shape, q.get_device()
-    if (dtype is not torch.bfloat16 and dtype is not torch.float32) or device < 0 or len(shape) != 4:
+    if dtype not in _CODES or device < 0 or len(shape) != 4:
         raise ValueError("q must be a bf16 or fp32 CUDA tensor [B, H, N, d]")
     B, H, N, d = shape
     Hk = 0
@@ -375,7 +376,7 @@ def _rope(fn_name, q, k, q_out, k_out, positions, frequencies, axes_dim, layout,
         tensors = (q, q_out, k, k_out)
     if q_out.shape != shape:
         raise ValueError("q, q_out must share one [B, H, N, d] shape")
-    strides = []
+    strides = ()
     for t in tensors:
         if t.dtype is not dtype or t.get_device() != device:
             raise ValueError("q, k and the outputs must have one dtype and device")
@@ -395,9 +396,9 @@ def _rope(fn_name, q, k, q_out, k_out, positions, frequencies, axes_dim, layout,
             or 2 * frequencies.numel() != sum(axes_dim):
         raise ValueError("frequencies must be a contiguous float64 CPU tensor of sum(axes_dim) / 2 values")
     _launch(fn_name, device, stream, (
-        q.data_ptr(), _ptr(k), q_out.data_ptr(), _ptr(k_out), (ctypes.c_longlong * len(strides))(*strides), positions.data_ptr(),
+        q.data_ptr(), _ptr(k), q_out.data_ptr(), _ptr(k_out), _TWELVE(*strides), positions.data_ptr(),
         0 if ps[0] == 1 else pb, pn, 32 if positions.dtype is torch.int32 else 64, frequencies.data_ptr(), _int_array(axes_dim),
-        len(axes_dim), B, H, Hk, N, d, BF16 if dtype is torch.bfloat16 else F32, layout, factor))
+        len(axes_dim), B, H, Hk, N, d, _CODES[dtype], layout, factor))
     return q_out if k is None else (q_out, k_out)
 
 
@@ -417,53 +418,53 @@ def clear_rope_bwd(dq_rot, dk_rot, dq, dk, positions, frequencies, axes_dim, lay
 def _norm_rows(x, *others):
     """(B, N, C), the dtype's code, the device's number and the (batch entry, row) strides of tensors [N, C] or [B, N, C] that share
     x's shape, dtype and device."""
-    import torch
-    shape, dtype, device = x.shape, x.dtype, x.get_device()
-    dims = len(shape)
-    if (dtype is not torch.bfloat16 and dtype is not torch.float32) or device < 0 or (dims != 3 and dims != 2):
+    shape, dtype, device, s = x.shape, x.dtype, x.get_device(), x.stride()
+    if dtype not in _CODES or device < 0 or not 2 <= len(s) <= 3:
         raise ValueError("x must be a bf16 or fp32 CUDA tensor [N, C] or [B, N, C]")
-    strides = []
-    for t in (x, *others):
+    last = shape[-1] > 1
+    if last and s[-1] != 1:
+        raise ValueError("the channels of a row must be contiguous")
+    strides = s[:2] if len(s) == 3 else (0, s[0])
+    for t in others:
         if t.dtype is not dtype or t.get_device() != device or t.shape != shape:
             raise ValueError("x, y and the gradients of rows must share one shape, dtype and device")
         s = t.stride()
-        if s[-1] != 1 and shape[-1] > 1:
+        if last and s[-1] != 1:
             raise ValueError("the channels of a row must be contiguous")
-        strides += s[:2] if dims == 3 else (0, s[0])
-    return shape if dims == 3 else (1, *shape), (BF16 if dtype is torch.bfloat16 else F32), device, strides
+        strides += s[:2] if len(s) == 3 else (0, s[0])
+    return shape if len(s) == 3 else (1, *shape), _CODES[dtype], device, strides
 
 
-def _norm_params(x, device, B, C, *params):
+def _norm_params(dtype, device, B, C, *params):
     """(dtype code, strides, numbers of axes seen) of weights and biases [C] or [B, C]; None stands for none."""
-    import torch
-    kind, strides, axes = None, [], set()
+    kind, strides, axes = None, (), 0
     for p in params:
         if p is None:
-            strides.append(0)
+            strides += (0,)
             continue
-        if kind is None:
+        s = p.stride()
+        if p.dtype is not kind:
+            code = _CODES.get(p.dtype)
+            if kind is not None or (code != F32 and code != dtype):
+                raise ValueError("weight, bias and their gradients must have one dtype, fp32 or that of x")
             kind = p.dtype
-            if kind is not torch.float32 and kind is not x.dtype:
-                raise ValueError("weight, bias and their gradients must be fp32 or of the dtype of x")
-        if p.dtype is not kind or p.get_device() != device:
-            raise ValueError("weight, bias and their gradients must have one dtype and the device of x")
-        s, shape = p.stride(), p.shape
-        if len(s) == 1 and shape[0] == C:
-            strides.append(0)
-        elif len(s) == 2 and shape[0] == B and shape[1] == C:
-            strides.append(s[0])
+        if p.get_device() != device:
+            raise ValueError("weight, bias and their gradients must be on the device of x")
+        if len(s) == 1 and p.shape[0] == C:
+            strides += (0,)
+        elif len(s) == 2 and p.shape == (B, C):
+            strides += s[:1]
         else:
             raise ValueError("weight, bias and their gradients must be [C] or [B, C]")
-        axes.add(len(s))
+        axes |= len(s)
         if s[-1] != 1 and C > 1:
             raise ValueError("the channels of a weight or bias must be contiguous")
-    return (BF16 if kind is torch.bfloat16 else F32), strides, axes
+    return (F32 if kind is None else _CODES[kind]), strides, axes
 
 
 def _norm_stats(device, n, *stats):
-    import torch
     for t in stats:
-        if t is not None and not (t.dtype is torch.float32 and t.get_device() == device and t.numel() == n and t.is_contiguous()):
+        if t is not None and (t.dtype is not torch.float32 or t.get_device() != device or t.numel() != n or not t.is_contiguous()):
             raise ValueError("mean and rstd must be contiguous fp32 tensors of a value a row on the device of x")
 
 
@@ -472,7 +473,7 @@ def clear_layer_norm_fwd(x, y, weight=None, bias=None, mean=None, rstd=None, wei
     (x - mean) * rstd * (weight_offset + weight) + bias, with weight and bias [C], or [B, C] for a pair a batch entry (a modulated
     layer: ``weight`` the scale, ``weight_offset`` 1, ``bias`` the shift).  ``mean``, ``rstd``: fp32, written for the backward pass."""
     (B, N, C), dtype, device, strides = _norm_rows(x, y)
-    kind, wb, _ = _norm_params(x, device, B, C, weight, bias)
+    kind, wb, _ = _norm_params(dtype, device, B, C, weight, bias)
     _norm_stats(device, B * N, mean, rstd)
     _launch("clear_layer_norm_fwd", device, stream, (
         x.data_ptr(), y.data_ptr(), _ptr(weight), _ptr(bias), _ptr(mean), _ptr(rstd), B, N, C, dtype, kind, *strides, *wb,
@@ -485,10 +486,10 @@ def clear_layer_norm_bwd(x, dy, weight, mean, rstd, dx, dweight=None, dbias=None
     or ``dy``) and, where given, ``dweight`` and ``dbias``, summed over all rows ([C]) or those of each batch entry ([B, C], as the
     weight is).  Returns the three."""
     (B, N, C), dtype, device, strides = _norm_rows(x, dy, dx)
-    kind, sums, axes = _norm_params(x, device, B, C, weight, dweight, dbias)
-    if len(axes) > 1:
+    kind, sums, axes = _norm_params(dtype, device, B, C, weight, dweight, dbias)
+    if axes == 3:
         raise ValueError("weight, dweight and dbias must all be [C] or all be [B, C]")
-    per_batch = 1 if 2 in axes else 0
+    per_batch = axes >> 1
     _norm_stats(device, B * N, mean, rstd)
     n_bytes = 0
     if dweight is not None or dbias is not None:

@@ -4,8 +4,10 @@
 //
 // HBM bounds it: x and dy in once, dx out once.  As in the forward kernel a thread owns 8 channels of a token and walks over its
 // (batch, head) rows, so sines and cosines are computed once a token; the gains' gradients stay in its registers all the while.
-// Device time, and bytes over the measured copy rate of 6541 GB/s: 4096 px bf16 380 us, 0.98; 1024 px bf16 31.9 us, 0.82 (4 us of it
-// the second kernel, which adds the blocks' sums of the gains' gradients), fp32 58 us, 0.90; the tiny fp32 shape 4.5 us.
+// Device time, and bytes over the measured copy rate of 6541 GB/s: 4096 px bf16 382 to 412 us by where the tensors
+// lie, 0.90 to 0.97; 1024 px bf16 32.0 us, 0.81 (4 us of it
+// the second kernel, which adds the blocks' sums of the gains' gradients), fp32 58 us, 0.90; the tiny fp32 shape 6.3 us.
+// 135 warp instructions for a warp's row of 8 channels a lane; fewer of them also means a higher clock under the board's power cap.
 #include <cooperative_groups.h>
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
@@ -42,19 +44,18 @@ struct PrepBwdParams {
 };
 
 // Rows come ahead by asynchronous copies of each thread's own channels into its own places of shared memory (bf16: 16 bytes, two
-// steps of three rows, 380 us at 4096 px where three rows ahead in registers take 410), or in registers where 8 channels are two
+// steps of three rows, 385 us at 4096 px where three rows ahead in registers take 410), or in registers where 8 channels are two
 // accesses (fp32, 4608 tokens of 24 heads, two rows: 58 us, copies 91).
 template <typename T> constexpr bool kAhead = sizeof(T) == 2;
 template <typename T> constexpr int kRowsOf = kAhead<T> ? 3 : 2;
-constexpr int kSteps = 2;
-template <typename T> constexpr int kRingBytes = kAhead<T> ? kSteps * kRowsOf<T> * 2 * kThreads * 16 : 0;
+template <typename T> constexpr int kRingBytes = kAhead<T> ? 2 * kRowsOf<T> * 2 * kThreads * 16 : 0;
 
 // Even warps have rows of Q, odd ones rows of K, so that a thread keeps one gain and one gain's gradient.
 template <typename T, int D>
 __global__ void __launch_bounds__(kThreads, kBlocksPerSm) clear_prep_bwd_kernel(const __grid_constant__ PrepBwdParams p)
 {
     constexpr int kLanes = D / kEpl, kTokens = 32 / kLanes, kPairs = kEpl / 2, kRows = kRowsOf<T>;
-    extern __shared__ __align__(16) unsigned char s_ring[];  // [kSteps][kRows][x, dy][kThreads][16]
+    extern __shared__ __align__(16) unsigned char s_ring[];  // two steps: [kRows][x, dy][kThreads][16]
     __shared__ float s_gain[kWarps][kTokens][D], s_sum[2 * D];
     __shared__ uint64_t s_turns[D / 2];
     __shared__ uint8_t s_axis[D / 2];
@@ -67,7 +68,7 @@ __global__ void __launch_bounds__(kThreads, kBlocksPerSm) clear_prep_bwd_kernel(
     const int w = warp & 1;
     const T *x_in = static_cast<const T *>(p.x[w]), *dy_in = static_cast<const T *>(p.dy[w]);
     T *dx_out = static_cast<T *>(p.dx[w]);
-    const F2 factor(p.factor[w]);
+    const float factor = p.factor[w];
     F2 gain[kPairs], dgain[kPairs];
 #pragma unroll
     for (int i = 0; i < kPairs; ++i) {
@@ -75,6 +76,7 @@ __global__ void __launch_bounds__(kThreads, kBlocksPerSm) clear_prep_bwd_kernel(
         dgain[i] = F2(0.f);
     }
     const long long stride = (long long)p.n_tokens * D;
+    const uint32_t ring = ptx::smem_u32(s_ring) + threadIdx.x * 16;
     const unsigned jobs = (p.n_tokens + kTokens - 1) / kTokens * p.parts;
     for (unsigned job = blockIdx.x * (kWarps / 2) + warp / 2; job < jobs; job += gridDim.x * (kWarps / 2)) {
         const unsigned grp = job / p.parts, raw = grp * kTokens + sub;
@@ -83,26 +85,28 @@ __global__ void __launch_bounds__(kThreads, kBlocksPerSm) clear_prep_bwd_kernel(
         const unsigned n = live ? raw : p.n_tokens - 1;  // the lanes stay together for the shuffles; what they add does not count
         const long long elem = (long long)n * D + c0;
         Pack<T, kEpl> nx[kRows], nd[kRows];
-        auto slot = [&](int step, int j, int which) {
-            return reinterpret_cast<T *>(s_ring + (((step * kRows + j) * 2 + which) * kThreads + threadIdx.x) * 16);
-        };
-        auto fetch = [&](int bh, int step) {
+        constexpr uint32_t kSlot = kThreads * 16, kStage = kRows * 2 * kSlot;
+        const T *x_at = x_in + elem + bh0 * stride, *dy_at = dy_in + elem + bh0 * stride;
+        T *dx_at = dx_out + elem + bh0 * stride;
+        int ahead = bh0;
+        auto fetch = [&](uint32_t to) {  // the next kRows rows, into a stage (by its offset in bytes)
 #pragma unroll
-            for (int j = 0; j < kRows; ++j)
-                if (bh + j < bh1) {
-                    const long long at = elem + (long long)(bh + j) * stride;
-                    if constexpr (kAhead<T>) {
-                        copy_async(ptx::smem_u32(slot(step, j, 0)), x_in + at);
-                        copy_async(ptx::smem_u32(slot(step, j, 1)), dy_in + at);
-                    } else {
-                        nx[j].load(x_in + at);
-                        nd[j].load(dy_in + at);
-                    }
+            for (int j = 0; j < kRows; ++j) {
+                const bool there = ahead + j < bh1;
+                if constexpr (kAhead<T>) {
+                    copy_async_if(ring + to + 2 * j * kSlot, x_at, there);
+                    copy_async_if(ring + to + (2 * j + 1) * kSlot, dy_at, there);
+                } else if (there) {
+                    nx[j].load(x_at);
+                    nd[j].load(dy_at);
                 }
+                x_at += stride;
+                dy_at += stride;
+            }
+            ahead += kRows;
             if constexpr (kAhead<T>) copies_commit();
         };
-#pragma unroll
-        for (int s = 0; s < (kAhead<T> ? kSteps - 1 : 1); ++s) fetch(bh0 + s * kRows, s);
+        fetch(0);
         int pos[3] = {0, 0, 0};
         if (n >= p.n_text) {
             pos[1] = (int)((n - p.n_text) / p.grid_w);
@@ -113,20 +117,23 @@ __global__ void __launch_bounds__(kThreads, kBlocksPerSm) clear_prep_bwd_kernel(
         for (int i = 0; i < kPairs; ++i) {
             const int axis = s_axis[c0 / 2 + i];
             turn_sincos(axis == 1 ? pos[1] : axis == 2 ? pos[2] : 0, s_turns[c0 / 2 + i], sn[i], cs[i]);
+            sn[i] *= factor;
+            cs[i] *= factor;
         }
-        int step = 0;
+        uint32_t stage = 0;
         for (int bh = bh0; bh < bh1; bh += kRows) {
             if constexpr (kAhead<T>) {
-                fetch(bh + (kSteps - 1) * kRows, step == 0 ? kSteps - 1 : step - 1);
-                copies_wait<kSteps - 1>();
+                fetch(stage ^ kStage);
+                copies_wait<1>();
             }
             F2 x2[kRows][kPairs], u2[kRows][kPairs];
             float ss[kRows], sx[kRows];
 #pragma unroll
             for (int j = 0; j < kRows; ++j) {
                 if constexpr (kAhead<T>) {  // beyond the last row: what lies there is not used
-                    nx[j].load(slot(step, j, 0));
-                    nd[j].load(slot(step, j, 1));
+                    const unsigned char *at = s_ring + stage + 2 * j * kSlot + threadIdx.x * 16;
+                    nx[j].load(reinterpret_cast<const T *>(at));
+                    nd[j].load(reinterpret_cast<const T *>(at + kSlot));
                 }
                 float x[kEpl], u[kEpl];
                 nx[j].get(x);
@@ -135,7 +142,7 @@ __global__ void __launch_bounds__(kThreads, kBlocksPerSm) clear_prep_bwd_kernel(
 #pragma unroll
                 for (int i = 0; i < kPairs; ++i) {
                     const float a = u[2 * i], b = u[2 * i + 1];
-                    u2[j][i] = F2(fmaf(b, sn[i], a * cs[i]), fmaf(-a, sn[i], b * cs[i])) * factor;
+                    u2[j][i] = F2(fmaf(b, sn[i], a * cs[i]), fmaf(-a, sn[i], b * cs[i]));
                     x2[j][i] = F2(x[2 * i], x[2 * i + 1]);
                     squares = fma2(x2[j][i], x2[j][i], squares);
                     products = fma2(u2[j][i] * gain[i], x2[j][i], products);
@@ -143,15 +150,20 @@ __global__ void __launch_bounds__(kThreads, kBlocksPerSm) clear_prep_bwd_kernel(
                 ss[j] = squares.lo() + squares.hi();
                 sx[j] = products.lo() + products.hi();
             }
-            if (++step == kSteps) step = 0;
-            if constexpr (!kAhead<T>) fetch(bh + kRows, 0);
+            stage ^= kStage;
+            if constexpr (!kAhead<T>) fetch(0);
+            // half of a row's lanes add up its squares, the others its products, and they swap
+            const bool second = lane & (kLanes / 2);
 #pragma unroll
-            for (int off = kLanes / 2; off > 0; off >>= 1)
+            for (int j = 0; j < kRows; ++j) {
+                float mine = second ? sx[j] : ss[j];
+                mine += __shfl_xor_sync(0xffffffffu, second ? ss[j] : sx[j], kLanes / 2);
 #pragma unroll
-                for (int j = 0; j < kRows; ++j) {
-                    ss[j] += __shfl_xor_sync(0xffffffffu, ss[j], off);
-                    sx[j] += __shfl_xor_sync(0xffffffffu, sx[j], off);
-                }
+                for (int off = kLanes / 4; off > 0; off >>= 1) mine += __shfl_xor_sync(0xffffffffu, mine, off);
+                const float other = __shfl_xor_sync(0xffffffffu, mine, kLanes / 2);
+                ss[j] = second ? other : mine;
+                sx[j] = second ? mine : other;
+            }
 #pragma unroll
             for (int j = 0; j < kRows; ++j) {
                 if (bh + j < bh1 && live) {
@@ -168,8 +180,9 @@ __global__ void __launch_bounds__(kThreads, kBlocksPerSm) clear_prep_bwd_kernel(
                     }
                     Pack<T, kEpl> out;
                     out.set(o);
-                    out.store(dx_out + elem + (long long)(bh + j) * stride);
+                    out.store(dx_at);
                 }
+                dx_at += stride;
             }
         }
         if constexpr (kAhead<T>) copies_wait<0>();

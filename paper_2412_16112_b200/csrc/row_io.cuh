@@ -117,11 +117,7 @@ struct Pack {
     }
 };
 
-// Asynchronous copy of 16 bytes into shared memory, and one that is made where `there` holds, without a branch.
-__device__ __forceinline__ void copy_async(uint32_t dst, const void *src)
-{
-    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
-}
+// Asynchronous copy of 16 bytes into shared memory where `there` holds, without a branch.
 __device__ __forceinline__ void copy_async_if(uint32_t dst, const void *src, bool there)
 {
     asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %2, 0;\n\t@p cp.async.cg.shared.global [%0], [%1], 16;\n\t}" ::"r"(dst), "l"(src),
